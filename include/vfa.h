@@ -338,6 +338,65 @@ int vfa_mxfp4_attn_noexp_fwd(const void* Q4, const void* QS, const void* K4, con
                              int use_minit, float softmax_scale, float descale_v, void* workspace,
                              size_t workspace_bytes, void* stream);
 
+/* ---- Serving from an 8-bit cache.  One step of a layer: vfa_qk_norm_rope_fwd (the projections of the new tokens), vfa_kv8_append (their
+ * keys and values into the cache), vfa_kv8_decode_fwd (their attention); a prompt takes vfa_qk_norm_rope_fwd, vfa_attn_fwd and
+ * vfa_kv8_append.
+ *
+ * The cache holds, for each batch entry and KV head, blocks of 64 tokens of keys and of values, each with E4M3 codes and one scale
+ * 2^(byte - 127); a code stands for its E4M3 value times that:
+ *   K8 [B, Hkv, n_cap / 64, d / 64, 64, 64]  codes of keys: feature half (d = 128), token, feature
+ *   V8 [B, Hkv, n_cap / 64, d, 64]           codes of values: feature, then token 16 t + 4 g + r of the block at place 16 g + 4 t + r
+ *   KS, VS [B, Hkv, n_cap / 64]              the scales' bytes
+ * (16-byte aligned codes; n_cap a multiple of 64, else VFA_ERR_UNSUPPORTED; B * Hkv <= 65535).  Nothing of a cache has to be set before its first
+ * rows are written.  Rewinding a sequence (drafts that were refused) is a smaller length in the next call.  Lengths are either one for all
+ * (ints), or DEVICE arrays of B ints, 4-byte aligned, read by the kernels and clamped to [0, n_cap].  Only d in {64, 128}. ---- */
+
+/* Norm, rotation and layout of projected queries, keys and values, one pass.
+ *   Xq [B, N, Hq, d], Xk, Xv [B, N, Hkv, d]  bf16, any strides (in elements, multiples of 8: batch, token, head), features contiguous
+ *   Q [B, Hq, N, d], K, V [B, Hkv, N, d]     bf16; the inputs and outputs may not overlap.  Xv and V may both be NULL
+ * Queries and keys: z = x * (mean(x^2) + eps)^(-1/2) * weight over the d features of a head (norm = 1; weights [d] bf16, each may be NULL for
+ * 1; eps >= 0) or z = x (norm = 0; no weights), then the first rot_dim features (a multiple of 16, 0 to d) are rotated in pairs i < rot_dim / 2,
+ * (i, i + rot_dim / 2) or, interleaved = 1, (2 i, 2 i + 1):  y_a = z_a cos - z_b sin, y_b = z_b cos + z_a sin, with cos and sin of the token's
+ * position from cos_sin [n_pos, rot_dim] fp32 (16-byte aligned; a row holds rot_dim / 2 cosines, then as many sines).  Token n of entry b has
+ * position first_pos[b] + n (DEVICE array; NULL: first + n), clamped to [0, n_pos - 1].  Values are copied.
+ * Computed in fp32 from the bf16 inputs, rounded to bf16 once. */
+int vfa_qk_norm_rope_fwd(const void* Xq, const void* Xk, const void* Xv, void* Q, void* K, void* V, int B, int N,
+                         int Hq, int Hkv, int d, long long q_sb, long long q_sn, long long q_sh, long long k_sb,
+                         long long k_sn, long long k_sh, long long v_sb, long long v_sn, long long v_sh, int norm,
+                         const void* q_weight, const void* k_weight, float eps, const float* cos_sin, int n_pos,
+                         int rot_dim, int interleaved, const int* first_pos, int first, void* stream);
+
+/* Writes new rows into the cache: sequence b gets rows 0, 1, ... of K, V [B, Hkv, n_in, d] (bf16, any strides in elements, multiples of 8:
+ * batch, head, token) as its tokens old_lens[b] <= n < new_lens[b] (n_in of them at most; none where old >= new), or all sequences as n_old <= n < n_new
+ * (both arrays NULL; VFA_ERR_INVALID_ARG unless 0 <= n_old <= n_new <= n_cap and n_new - n_old <= n_in).
+ * The scale of a block that holds no token before the new ones is 2^e with the smallest e >= -117 for which the largest finite magnitude of its new
+ * elements is at most 448 * 2^e; of one that does, the larger of that and its old scale, and if that is not the old one the tokens before
+ * are coded again.  A code is x * 2^-e rounded to nearest even, infinities at +-448, NaN as NaN.  Tokens behind the new ones are left as they were. */
+int vfa_kv8_append(const void* K, const void* V, void* K8, void* V8, void* KS, void* VS, int B, int Hkv, int n_cap,
+                   int n_in, int d, long long k_sb, long long k_sh, long long k_sn, long long v_sb, long long v_sh,
+                   long long v_sn, const int* old_lens, const int* new_lens, int n_old, int n_new, void* stream);
+
+/* Reads the first n tokens of every sequence back: K, V [B, Hkv, n, d] bf16 (code times scale, rounded to bf16, which only makes infinities of
+ * what is above its range); zeros for tokens at and behind seq_lens[b] (NULL: seq_len). */
+int vfa_kv8_read(const void* K8, const void* V8, const void* KS, const void* VS, void* K, void* V, int B, int Hkv,
+                 int n_cap, int n, int d, const int* seq_lens, int seq_len, void* stream);
+
+/* A number of key ranges for vfa_kv8_decode_fwd that suits a batch of sequences of up to n_keys tokens. */
+int vfa_kv8_decode_splits(int B, int Hkv, int n_keys);
+
+/* Bytes of workspace vfa_kv8_decode_fwd needs for n_splits > 1. */
+size_t vfa_kv8_decode_workspace_bytes(int B, int Hq, int n_q, int d, int n_splits);
+
+/* Attention of each sequence's n_q newest tokens (1: a decode step; more: drafted tokens, or the last of a prompt) over its cache, which holds
+ * them already.  Q, O [B, Hq, n_q, d] bf16, LSE [B, Hq, n_q] fp32 or NULL.  Sequence b has L = seq_lens[b] tokens (NULL: n_keys), and its token t of the
+ * n_q sees the first L - n_q + 1 + t of them; a token that sees none (L < n_q) gets O = 0, LSE = -inf.  Exact attention over the values that
+ * the cache stands for: products of bf16 queries with them and sums in fp32, softmax in fp32, weights rounded to bf16 for the product with V.
+ * (Hq / Hkv) * n_q <= 32, else VFA_ERR_UNSUPPORTED.  n_splits as in vfa_decode_varlen_fwd (1 to 4096; vfa_kv8_decode_splits suggests one);
+ * the workspace, 16-byte aligned, contents irrelevant, is used for n_splits > 1 only.  Calls that may run at the same time need workspaces of their own. */
+int vfa_kv8_decode_fwd(const void* Q, const void* K8, const void* V8, const void* KS, const void* VS, void* O, float* LSE,
+                       int B, int Hq, int Hkv, int n_cap, int n_q, int d, const int* seq_lens, int n_keys, int n_splits,
+                       float softmax_scale, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Static string for a return code. */
 const char* vfa_strerror(int code);
 

@@ -9,7 +9,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libvfa.so")
 BINDING = os.path.join(HERE, "_native.so")
-SOURCES = ["vfa_fwd.hip", "vsa_pp.hip"]
+SOURCES = ["vfa_fwd.hip", "vsa_pp.hip", "serving.hip"]
 # attn_vsa_pp_kernel sits at the register limit; with the scheduler's default register-pressure tracking the allocator
 # spills an accumulator inside its steady loops, with this tracker it does not (checked on the generated code)
 EXTRA_FLAGS = {"vsa_pp.hip": ["-mllvm", "-amdgpu-use-amdgpu-trackers=1"]}

@@ -184,6 +184,8 @@ PyMethodDef methods[] = {
     VFA_METHOD(vfa_decode_workspace_bytes), VFA_METHODS(vfa_decode_fwd), VFA_METHODS(vfa_decode_noalloc_fwd), VFA_METHODS(vfa_decode_varlen_fwd),
     VFA_METHODS(vfa_fp8_quantize), VFA_METHOD(vfa_fp8_v_bytes), VFA_METHODS(vfa_fp8_pack_v), VFA_METHODS(vfa_fp8_attn_fwd), VFA_METHODS(vfa_fp8_attn_noexp_fwd),
     VFA_METHODS(vfa_mxfp4_quantize), VFA_METHOD(vfa_mxfp4_workspace_bytes), VFA_METHODS(vfa_mxfp4_attn_fwd), VFA_METHODS(vfa_mxfp4_attn_noexp_fwd),
+    VFA_METHODS(vfa_qk_norm_rope_fwd), VFA_METHODS(vfa_kv8_append), VFA_METHODS(vfa_kv8_read), VFA_METHOD(vfa_kv8_decode_splits),
+    VFA_METHOD(vfa_kv8_decode_workspace_bytes), VFA_METHODS(vfa_kv8_decode_fwd),
     {"check_qkv", VFA_FUNCTION(check_qkv)}, {"check_cache", VFA_FUNCTION(check_cache)},
     {"bytes_of", &bytes_of, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};

@@ -289,7 +289,8 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 2 : 1) void decode_split_kernel(c
 // ranges and 6.3 us for 128 heads of 16, a chain of load latencies; with loads behind branches and a division in front this took 3.0 and
 // 5.0, now 2.7 and 4.8.  Only the rounds that the ranges fill: steps of 6400 heads of two ranges of 100 keys, four rounds of loads for
 // each / one, d = 64 16.8 / 14.4, d = 128 29.2 / 26.8.)
-template <int D, bool DEALT>
+// (NANS: a row whose sum is NaN has that for its LSE, not -inf)
+template <int D, bool DEALT, bool NANS = false>
 __global__ __launch_bounds__(256) void decode_merge_kernel(const DecodeParams p) {
     constexpr int C4 = D / 4, NG = 256 / C4;
     __shared__ float xo[NG][D], xm[NG], xl[NG];
@@ -362,9 +363,10 @@ __global__ __launch_bounds__(256) void decode_merge_kernel(const DecodeParams p)
         o0 += a * xo[k][2 * t];
         o1 += a * xo[k][2 * t + 1];
     }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const bool sum = NANS ? l != 0.f : l > 0.f;
+    const float inv = sum ? 1.f / l : 0.f;
     *reinterpret_cast<uint32_t*>(p.O + (size_t)row * D + 2 * t) = pack_bf16(o0 * inv, o1 * inv);
-    if (p.LSE && t == 0) p.LSE[row] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    if (p.LSE && t == 0) p.LSE[row] = sum ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
 }  // namespace

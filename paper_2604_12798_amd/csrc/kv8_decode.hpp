@@ -1,0 +1,273 @@
+// Attention of each sequence's newest tokens over the 8-bit cache.
+#pragma once
+#include "decode.hpp"
+#include "kv8.hpp"
+
+namespace {
+
+// ---------------------------------------------------------------------------------------------
+// The rows of a KV head, its query heads' n_q newest tokens (at most 32), are the columns of the score tile, 16 to a tile (RT tiles):
+//   S^T [64 keys, rows] = K Q^T            v_mfma_f32_16x16x32_bf16, keys 16 at a time
+//   O^T [D, rows] += V^T P^T               the same, features 16 at a time
+// K and V go from memory to registers as codes and are converted there (v_cvt_scalef32_pk_bf16_fp8, the block's power of two inside it: exact).
+// In the accumulators lane (row, g) of a score tile holds keys 16 t + 4 g + r, r = 0..3, of the four key groups t: as the B operand of P V that is
+// what lane group g needs, if the A operand has the same keys in the same order, which is how the cache lays out V.  So neither K, V nor P
+// passes through LDS; only the waves' results meet there.  A wave requests a tile's keys when those of the one before are converted and its
+// values likewise, so that 8 to 16 KiB (D = 128) are on their way to each wave all the time.
+// Token t of the n_q sees keys < len - n_q + 1 + t.  What lies behind a sequence's end is neither a key (its scores are -inf) nor a value (its
+// codes are cleared: 0 * NaN).  A NaN in the value of a key that only some of the tokens see would reach the others through weights of zero:
+// where there is one, each token has its own product (with the keys that it does not see cleared).
+// Partial sums of ranges and their merge: decode.hpp, a row for a head.
+struct Kv8Decode {
+    DecodeParams d;  // Hq, g: rows for heads (query heads times new tokens); K, V not used
+    const uint8_t* K8;
+    const uint8_t* V8;
+    const uint8_t* KS;
+    const uint8_t* VS;
+    int T, n_q;
+};
+
+// eight codes -> bf16 values
+__device__ __forceinline__ bf16x8 kv8_bf16x8(uint32_t w0, uint32_t w1, float scale) {
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, true);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+__device__ __forceinline__ float kg_max(float x) {  // over the four lanes of a row
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return xhalf_max(fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1])));
+}
+__device__ __forceinline__ float kg_sum(float x) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return xhalf_sum(__uint_as_float(a[0]) + __uint_as_float(a[1]));
+}
+// A block's codes: bytes 1024 u + off of it, u = 0..NI - 1; with `bytes` = 0 zeros, and no access.
+template <int NI>
+__device__ __forceinline__ void kv8_request(const uint8_t* base, int bytes, uint32_t off, u32x4* r) {
+    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+#pragma unroll
+    for (int u = 0; u < NI; ++u) r[u] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, off, u * 1024, 2));
+}
+
+template <int D, int RT, int W, int LENS>
+__global__ __launch_bounds__(64 * W, RT == 1 ? 3 : 2) void kv8_decode_kernel(const Kv8Decode P) {
+    const DecodeParams& p = P.d;
+    constexpr int S = D / 64, DT = D / 16, NI = D / 16, BYTES = BN * D;
+    constexpr int OROW = D + 4, WS = 16 * RT * OROW + 32 * RT;  // floats of a row, of a wave's part of the exchange
+    __shared__ __attribute__((aligned(16))) float ex[W * WS];
+    const int lane = threadIdx.x & 63, ql = lane & 15, kg = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int rows = p.g, hkv = LENS == LENS_FIXED ? blockIdx.y : blockIdx.z;
+    int b = LENS == LENS_FIXED ? blockIdx.z : blockIdx.y, r = blockIdx.x, nb = p.n_splits;
+    const int w = b * p.n_splits + r;  // range of the batch's list
+    if (LENS == LENS_DEALT) {
+        const Ranges rg = varlen_find(p, lane, w, 0);
+        if (rg.b < 0) return;  // (the same in all waves of the workgroup)
+        b = rg.b; r = w - rg.first; nb = rg.nb;
+    }
+    const size_t slot = (size_t)w * p.Hq + hkv * rows;
+    const int len = LENS == LENS_ONE ? p.n_keys : __builtin_amdgcn_readfirstlane(min(max(p.seq_lens[b], 0), p.n_cap));
+    const int Tc = (len + BN - 1) / BN, per = (Tc + nb - 1) / nb;
+    const int r0 = r * per, r1 = min(Tc, r0 + per);
+    const size_t bh = (size_t)b * p.Hkv + hkv;
+    const uint8_t* const K8 = P.K8 + bh * P.T * BYTES;
+    const uint8_t* const V8 = P.V8 + bh * P.T * BYTES;
+    const uint8_t* const KS = P.KS + bh * P.T;
+    const uint8_t* const VS = P.VS + bh * P.T;
+    const uint32_t off = ql * 64 + kg * 16;
+    bf16x8 qf[RT][2 * S];
+    int sees[RT];  // keys that the lane's rows see
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int row = min(16 * rt + ql, rows - 1);
+        const uint16_t* const q = p.Q + ((size_t)b * p.Hq + hkv * rows + row) * D;
+#pragma unroll
+        for (int s = 0; s < 2 * S; ++s) qf[rt][s] = *reinterpret_cast<const bf16x8*>(q + 64 * (s >> 1) + 16 * kg + 8 * (s & 1));
+        sees[rt] = len - P.n_q + 1 + row % P.n_q;
+    }
+    const int all_see = len - P.n_q + 1;  // keys below are seen by every row
+    f32x4 ot[RT][DT];
+    float m2[RT], lsum[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        m2[rt] = -INFINITY;
+        lsum[rt] = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) ot[rt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    u32x4 rk[NI], rv[NI];
+    int sk = 0, sv = 0;
+    auto want = [&](int t) { return t < r1 ? BYTES : 0; };
+    auto request_k = [&](int t) __attribute__((always_inline)) {
+        sk = KS[min(t, r1 - 1)];
+        kv8_request<NI>(K8 + (size_t)t * BYTES, want(t), off, rk);
+    };
+    auto request_v = [&](int t) __attribute__((always_inline)) {
+        sv = VS[min(t, r1 - 1)];
+        kv8_request<NI>(V8 + (size_t)t * BYTES, want(t), off, rv);
+    };
+    // tile t; EDGE: some row does not see all of it
+    auto body = [&](int t, auto edge_c) __attribute__((always_inline)) {
+        constexpr bool EDGE = decltype(edge_c)::value;
+        f32x4 st[RT][4];
+        const float ks = ldexpf(1.f, sk - 127);
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) st[rt][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                const u32x4 x = rk[4 * s + kt];
+                const bf16x8 k0 = kv8_bf16x8(x[0], x[1], ks), k1 = kv8_bf16x8(x[2], x[3], ks);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    st[rt][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qf[rt][2 * s], st[rt][kt], 0, 0, 0);
+                    st[rt][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qf[rt][2 * s + 1], st[rt][kt], 0, 0, 0);
+                }
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);  // (requests go out where they are written)
+        request_k(t + W);
+        __builtin_amdgcn_sched_barrier(0);
+        const int key0 = t * BN;
+        bf16x8 pf[RT][2];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            if (EDGE) {
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (key0 + 16 * kt + 4 * kg + e >= sees[rt]) st[rt][kt][e] = -INFINITY;
+            }
+            float mx = -INFINITY;
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) mx = fmaxf(mx, st[rt][kt][e]);
+            const float m_new = fmaxf(m2[rt], kg_max(mx) * p.c);
+            const float msub = finite_max(m_new);
+            if (__builtin_amdgcn_ballot_w64(m_new != m2[rt]) != 0) {
+                const float alpha = __builtin_amdgcn_exp2f(m2[rt] - msub);
+                lsum[rt] *= alpha;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) ot[rt][dt] *= alpha;
+                m2[rt] = m_new;
+            }
+            uint32_t pk[8];
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt) {
+                float e4[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    e4[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[rt][kt][e], p.c, -msub));
+                    lsum[rt] += e4[e];
+                }
+                pk[2 * kt] = pack_bf16(e4[0], e4[1]);
+                pk[2 * kt + 1] = pack_bf16(e4[2], e4[3]);
+            }
+            pf[rt][0] = __builtin_bit_cast(bf16x8, u32x4{pk[0], pk[1], pk[2], pk[3]});
+            pf[rt][1] = __builtin_bit_cast(bf16x8, u32x4{pk[4], pk[5], pk[6], pk[7]});
+        }
+        const float vs = ldexpf(1.f, sv - 127);
+        // the keys of the lane's bytes below `end`: dword kt holds keys 16 kt + 4 kg + (0..3)
+        auto seen_bytes = [&](int kt, int end) {
+            const int left = end - (key0 + 16 * kt + 4 * kg);
+            return left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << 8 * left) - 1;
+        };
+        bool apart = false;  // tokens have a product each
+        if (EDGE) {
+            uint32_t nan = 0;
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt) {
+                const uint32_t in = seen_bytes(kt, len), some = in & ~seen_bytes(kt, all_see);
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) {
+                    rv[dt][kt] &= in;
+                    nan |= ((rv[dt][kt] & some & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+                }
+            }
+            apart = __builtin_amdgcn_ballot_w64(nan != 0) != 0;
+        }
+        if (!apart) {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                const bf16x8 v0 = kv8_bf16x8(rv[dt][0], rv[dt][1], vs), v1 = kv8_bf16x8(rv[dt][2], rv[dt][3], vs);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    ot[rt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pf[rt][0], ot[rt][dt], 0, 0, 0);
+                    ot[rt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pf[rt][1], ot[rt][dt], 0, 0, 0);
+                }
+            }
+        } else {
+            for (int tok = 0; tok < P.n_q; ++tok) {
+                const int end = all_see + tok;
+                const uint32_t c0 = seen_bytes(0, end), c1 = seen_bytes(1, end), c2 = seen_bytes(2, end), c3 = seen_bytes(3, end);
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) {
+                    const bf16x8 v0 = kv8_bf16x8(rv[dt][0] & c0, rv[dt][1] & c1, vs), v1 = kv8_bf16x8(rv[dt][2] & c2, rv[dt][3] & c3, vs);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) {
+                        f32x4 o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pf[rt][0], ot[rt][dt], 0, 0, 0);
+                        o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pf[rt][1], o, 0, 0, 0);
+                        if (sees[rt] == end) ot[rt][dt] = o;
+                    }
+                }
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        request_v(t + W);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    int t = r0 + wave;
+    if (t < r1) {
+        request_k(t);
+        request_v(t);
+        const int whole = all_see < 0 ? 0 : all_see / BN;  // tiles below are seen whole by every row
+        for (; t < min(r1, whole); t += W) body(t, std::false_type{});
+        for (; t < r1; t += W) body(t, std::true_type{});
+    }
+    // the waves' sums meet in LDS
+    float* const ox = ex + wave * WS;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const float l = kg_sum(lsum[rt]);
+        const int row = 16 * rt + ql;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(ox + row * OROW + 16 * dt + 4 * kg) = ot[rt][dt];
+        if (kg == 0) {
+            ox[16 * RT * OROW + row] = m2[rt];
+            ox[16 * RT * OROW + 16 * RT + row] = l;
+        }
+    }
+    __syncthreads();
+    for (int idx = threadIdx.x; idx < rows * (D / 4); idx += 64 * W) {
+        const int col = idx / (D / 4), c4 = idx - col * (D / 4);
+        float m = -INFINITY;
+#pragma unroll
+        for (int v = 0; v < W; ++v) m = fmaxf(m, ex[v * WS + 16 * RT * OROW + col]);
+        const float msub = finite_max(m);
+        float lt = 0.f;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int v = 0; v < W; ++v) {
+            const float a = __builtin_amdgcn_exp2f(ex[v * WS + 16 * RT * OROW + col] - msub);
+            lt += a * ex[v * WS + 16 * RT * OROW + 16 * RT + col];
+            o += a * *reinterpret_cast<const f32x4*>(ex + v * WS + col * OROW + 4 * c4);
+        }
+        if (p.n_splits == 1) {  // the only range: this is the result
+            const size_t row = (size_t)b * p.Hq + hkv * rows + col;
+            const float inv = lt == 0.f ? 0.f : 1.f / lt;
+            *reinterpret_cast<u32x2*>(p.O + row * D + 4 * c4) = u32x2{pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
+            if (p.LSE && c4 == 0) p.LSE[row] = lt == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(lt)) * kLn2;
+        } else {
+            *reinterpret_cast<f32x4*>(p.opart + (slot + col) * D + 4 * c4) = o;
+            if (c4 == 0) {
+                p.pm[slot + col] = m;
+                p.lpart[slot + col] = lt;
+            }
+        }
+    }
+}
+
+}  // namespace

@@ -1,0 +1,126 @@
+// Norms of queries and keys for each head, the rotation by position, and the head-major layout of the attention calls, in one pass.
+#pragma once
+#include "common.hpp"
+
+namespace {
+
+// ---------------------------------------------------------------------------------------------
+// A row (one head of one token) x of D features becomes
+//   z = x * (mean(x^2) + eps)^(-1/2) * w                    (queries and keys; NORM)
+//   y_a = z_a cos - z_b sin,  y_b = z_b cos + z_a sin       (pair i < rot / 2 of features: (i, i + rot / 2) or (2 i, 2 i + 1); PAIRS)
+// in 32 bits, rounded once.  Values are copied.  D / 16 lanes hold a row, 16 features each: the two halves of eight pairs, so that the
+// rotation needs no other lane, and the sum of squares log2(D / 16) steps of DPP.
+enum Pairs { PAIRS_NONE = 0, PAIRS_HALF = 1, PAIRS_NEXT = 2 };
+struct RopeParams {
+    const uint16_t* X[3];    // queries, keys, values [B, N, heads, D] with strides (elements); values may be null
+    long long sb[3], sn[3], sh[3];
+    uint16_t* Y[3];          // [B, heads, N, D]
+    const uint16_t* W[2];    // [D] or null
+    const float* cos_sin;    // [n_pos, rot]: rot / 2 cosines, then as many sines
+    const int* first_pos;    // [B] or null
+    int first, n_pos, rot, N, tokens;  // tokens = B * N
+    int Hq, Hkv, heads;      // heads = Hq + Hkv (+ Hkv with values)
+    int per;                 // heads that a workgroup does one after the other
+    float eps;
+};
+
+__device__ __forceinline__ void unpack_bf16(const u32x4& r, float* v) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        v[2 * e] = __uint_as_float(r[e] << 16);
+        v[2 * e + 1] = __uint_as_float(r[e] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ u32x4 pack_bf16x8(const float* v) {
+    return u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+}
+// Sum over the D / 16 lanes of a row: neighbours, pairs, quads.
+template <int D>
+__device__ __forceinline__ float row_sum(float x) {
+    auto add = [](float a, auto ctrl) {
+        return a + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, a), decltype(ctrl)::value, 0xf, 0xf, false));
+    };
+    x = add(x, std::integral_constant<int, 0xb1>{});             // quad_perm [1, 0, 3, 2]
+    x = add(x, std::integral_constant<int, 0x4e>{});             // quad_perm [2, 3, 0, 1]
+    if (D == 128) x = add(x, std::integral_constant<int, 0x141>{});  // row_half_mirror: the other quad of the eight
+    return x;
+}
+
+template <int D, bool NORM, int PAIRS>
+__global__ __launch_bounds__(256) void norm_rope_kernel(const RopeParams p) {
+    constexpr int L = D / 16, ROWS = 256 / L;  // lanes of a row; tokens of a workgroup
+    const int j = threadIdx.x % L;
+    const long long tok = (long long)blockIdx.x * ROWS + threadIdx.x / L;
+    const bool live = tok < p.tokens;
+    const int t = (int)(live ? tok : p.tokens - 1), b = t / p.N, n = t - b * p.N;
+    // chunks of eight features: the two halves of eight pairs, or two neighbours
+    const int pairs8 = PAIRS == PAIRS_NONE ? 0 : p.rot / 16;
+    int ca = 2 * j, cb = 2 * j + 1;
+    if (PAIRS == PAIRS_HALF && j < pairs8) { ca = j; cb = j + pairs8; }
+    float cs[8], sn[8];
+    if (PAIRS != PAIRS_NONE) {
+        const int pos = (int)min(max((long long)n + (p.first_pos ? p.first_pos[b] : p.first), 0LL), (long long)p.n_pos - 1);
+        const float* const c = p.cos_sin + (size_t)pos * p.rot;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            cs[e] = j < pairs8 ? c[8 * j + e] : 1.f;
+            sn[e] = j < pairs8 ? c[p.rot / 2 + 8 * j + e] : 0.f;
+        }
+    }
+    const int h1 = min(p.heads, ((int)blockIdx.y + 1) * p.per);
+    for (int hh = blockIdx.y * p.per; hh < h1; ++hh) {
+        const int kind = hh < p.Hq ? 0 : hh < p.Hq + p.Hkv ? 1 : 2;  // (the same in all lanes)
+        const int h = kind == 0 ? hh : kind == 1 ? hh - p.Hq : hh - p.Hq - p.Hkv, H = kind == 0 ? p.Hq : p.Hkv;
+        const uint16_t* const x = p.X[kind] + b * p.sb[kind] + n * p.sn[kind] + h * p.sh[kind];
+        uint16_t* const y = p.Y[kind] + (((size_t)b * H + h) * p.N + n) * D;
+        u32x4 ra = *reinterpret_cast<const u32x4*>(x + 8 * ca), rb = *reinterpret_cast<const u32x4*>(x + 8 * cb);
+        if (kind < 2) {
+            float a[8], c[8];
+            unpack_bf16(ra, a);
+            unpack_bf16(rb, c);
+            if (NORM) {
+                float ss = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) ss += a[e] * a[e] + c[e] * c[e];
+                const float r = 1.f / sqrtf(row_sum<D>(ss) * (1.f / D) + p.eps);
+                const uint16_t* const w = p.W[kind];
+                float wa[8], wb[8];
+                if (w) {
+                    unpack_bf16(*reinterpret_cast<const u32x4*>(w + 8 * ca), wa);
+                    unpack_bf16(*reinterpret_cast<const u32x4*>(w + 8 * cb), wb);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    a[e] *= w ? r * wa[e] : r;
+                    c[e] *= w ? r * wb[e] : r;
+                }
+            }
+            if (PAIRS == PAIRS_HALF) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float za = a[e], zb = c[e];
+                    a[e] = za * cs[e] - zb * sn[e];
+                    c[e] = zb * cs[e] + za * sn[e];
+                }
+            } else if (PAIRS == PAIRS_NEXT) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float z0 = a[2 * e], z1 = a[2 * e + 1];
+                    a[2 * e] = z0 * cs[e] - z1 * sn[e];
+                    a[2 * e + 1] = z1 * cs[e] + z0 * sn[e];
+                    z0 = c[2 * e]; z1 = c[2 * e + 1];
+                    c[2 * e] = z0 * cs[4 + e] - z1 * sn[4 + e];
+                    c[2 * e + 1] = z1 * cs[4 + e] + z0 * sn[4 + e];
+                }
+            }
+            ra = pack_bf16x8(a);
+            rb = pack_bf16x8(c);
+        }
+        if (live) {
+            *reinterpret_cast<u32x4*>(y + 8 * ca) = ra;
+            *reinterpret_cast<u32x4*>(y + 8 * cb) = rb;
+        }
+    }
+}
+
+}  // namespace

@@ -1,0 +1,201 @@
+// C ABI of the serving operators around the 8-bit cache (declared in vfa.h): argument checks, kernel selection and launches.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+#include <math.h>
+
+#include "vfa.h"
+
+#include "common.hpp"
+#include "host.hpp"
+#include "norm_rope.hpp"
+#include "kv8.hpp"
+#include "kv8_decode.hpp"
+
+namespace {
+
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+int launched() { return hipGetLastError() == hipSuccess ? VFA_OK : VFA_ERR_HIP; }
+
+// What the cache's entry points have in common; *done: there is nothing to do.
+int check_cache8(const void* K8, const void* V8, const void* KS, const void* VS, int B, int Hkv, int n_cap, int d, bool* done) {
+    *done = false;
+    if (B < 0 || Hkv <= 0 || n_cap < 0 || d <= 0) return VFA_ERR_INVALID_ARG;
+    if ((d != 64 && d != 128) || n_cap % BN != 0) return VFA_ERR_UNSUPPORTED;
+    if (B == 0) { *done = true; return VFA_OK; }
+    if (n_cap > 0 && (!K8 || !V8 || !KS || !VS || !aligned16(K8) || !aligned16(V8))) return VFA_ERR_INVALID_ARG;
+    if (2LL * Hkv > 65535 || (long long)B * Hkv > 65535) return VFA_ERR_UNSUPPORTED;
+    return VFA_OK;
+}
+
+// Strides of rows that are read 16 bytes at a time
+bool whole_runs(long long a, long long b, long long c) { return ((a | b | c) & 7) == 0; }
+
+template <typename F>
+void with_d(int d, F f) {
+    if (d == 128) f(std::integral_constant<int, 128>{});
+    else f(std::integral_constant<int, 64>{});
+}
+
+}  // namespace
+
+extern "C" {
+
+int vfa_qk_norm_rope_fwd(const void* Xq, const void* Xk, const void* Xv, void* Q, void* K, void* V, int B, int N, int Hq, int Hkv, int d,
+                         long long q_sb, long long q_sn, long long q_sh, long long k_sb, long long k_sn, long long k_sh, long long v_sb,
+                         long long v_sn, long long v_sh, int norm, const void* q_weight, const void* k_weight, float eps,
+                         const float* cos_sin, int n_pos, int rot_dim, int interleaved, const int* first_pos, int first, void* stream) {
+    if (B < 0 || N < 0 || Hq <= 0 || Hkv <= 0 || d <= 0 || rot_dim < 0) return VFA_ERR_INVALID_ARG;
+    if ((norm != 0 && norm != 1) || (interleaved != 0 && interleaved != 1)) return VFA_ERR_INVALID_ARG;
+    if (d != 64 && d != 128) return VFA_ERR_UNSUPPORTED;
+    if (rot_dim > d || rot_dim % 16 != 0) return VFA_ERR_INVALID_ARG;
+    if (norm ? !(eps >= 0.f) || !isfinite(eps) : q_weight || k_weight) return VFA_ERR_INVALID_ARG;
+    if (rot_dim > 0 && (!cos_sin || !aligned16(cos_sin) || n_pos <= 0 || !aligned4(first_pos))) return VFA_ERR_INVALID_ARG;
+    if (B == 0 || N == 0) return VFA_OK;
+    if (!Xq || !Xk || !Q || !K || !Xv != !V) return VFA_ERR_INVALID_ARG;
+    if (!aligned16(Xq) || !aligned16(Xk) || !aligned16(Xv) || !aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(q_weight) ||
+        !aligned16(k_weight))
+        return VFA_ERR_INVALID_ARG;
+    if (!whole_runs(q_sb, q_sn, q_sh) || !whole_runs(k_sb, k_sn, k_sh) || (V && !whole_runs(v_sb, v_sn, v_sh))) return VFA_ERR_INVALID_ARG;
+    RopeParams p{};
+    p.X[0] = (const uint16_t*)Xq; p.X[1] = (const uint16_t*)Xk; p.X[2] = (const uint16_t*)Xv;
+    p.Y[0] = (uint16_t*)Q; p.Y[1] = (uint16_t*)K; p.Y[2] = (uint16_t*)V;
+    p.sb[0] = q_sb; p.sn[0] = q_sn; p.sh[0] = q_sh;
+    p.sb[1] = k_sb; p.sn[1] = k_sn; p.sh[1] = k_sh;
+    p.sb[2] = v_sb; p.sn[2] = v_sn; p.sh[2] = v_sh;
+    p.W[0] = (const uint16_t*)q_weight; p.W[1] = (const uint16_t*)k_weight;
+    p.cos_sin = cos_sin; p.first_pos = first_pos; p.first = first; p.n_pos = n_pos; p.rot = rot_dim;
+    const long long heads = (long long)Hq + Hkv + (V ? Hkv : 0), tokens = (long long)B * N;
+    if (tokens > 0x7fffffffLL || heads > 0x7fffffffLL) return VFA_ERR_UNSUPPORTED;
+    p.N = N; p.tokens = (int)tokens; p.Hq = Hq; p.Hkv = Hkv; p.heads = (int)heads; p.eps = eps;
+    const int rows = 256 / (d / 16);
+    const long long wgs = (tokens + rows - 1) / rows;
+    p.per = 4;
+    const long long ys = (heads + p.per - 1) / p.per;
+    if (ys > 65535 || wgs * ys > kMaxWorkgroups256) return VFA_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)wgs, (unsigned)ys);
+    hipStream_t s = (hipStream_t)stream;
+    (void)hipGetLastError();
+    with_d(d, [&](auto d_c) {
+        constexpr int D = decltype(d_c)::value;
+        auto launch = [&](auto norm_c) {
+            constexpr bool NORM = decltype(norm_c)::value;
+            if (rot_dim == 0) norm_rope_kernel<D, NORM, PAIRS_NONE><<<grid, 256, 0, s>>>(p);
+            else if (interleaved) norm_rope_kernel<D, NORM, PAIRS_NEXT><<<grid, 256, 0, s>>>(p);
+            else norm_rope_kernel<D, NORM, PAIRS_HALF><<<grid, 256, 0, s>>>(p);
+        };
+        if (norm) launch(std::true_type{});
+        else launch(std::false_type{});
+    });
+    return launched();
+}
+
+int vfa_kv8_append(const void* K, const void* V, void* K8, void* V8, void* KS, void* VS, int B, int Hkv, int n_cap, int n_in, int d,
+                   long long k_sb, long long k_sh, long long k_sn, long long v_sb, long long v_sh, long long v_sn, const int* old_lens,
+                   const int* new_lens, int n_old, int n_new, void* stream) {
+    bool done;
+    const int rc = check_cache8(K8, V8, KS, VS, B, Hkv, n_cap, d, &done);
+    if (rc != VFA_OK || n_in < 0) return rc != VFA_OK ? rc : VFA_ERR_INVALID_ARG;
+    if (!old_lens != !new_lens || !aligned4(old_lens) || !aligned4(new_lens)) return VFA_ERR_INVALID_ARG;
+    if (!old_lens && (n_old < 0 || n_old > n_new || n_new > n_cap || n_new - n_old > n_in)) return VFA_ERR_INVALID_ARG;
+    if (done || n_cap == 0 || n_in == 0 || (!old_lens && n_old == n_new)) return VFA_OK;
+    if (!K || !V || !aligned16(K) || !aligned16(V) || !whole_runs(k_sb, k_sh, k_sn) || !whole_runs(v_sb, v_sh, v_sn)) return VFA_ERR_INVALID_ARG;
+    Kv8Append p{};
+    p.X[0] = (const uint16_t*)K; p.X[1] = (const uint16_t*)V;
+    p.sb[0] = k_sb; p.sh[0] = k_sh; p.sn[0] = k_sn;
+    p.sb[1] = v_sb; p.sh[1] = v_sh; p.sn[1] = v_sn;
+    p.C[0] = (uint8_t*)K8; p.C[1] = (uint8_t*)V8; p.S[0] = (uint8_t*)KS; p.S[1] = (uint8_t*)VS;
+    p.old_lens = old_lens; p.new_lens = new_lens; p.old_len = n_old; p.new_len = n_new;
+    p.n_in = n_in; p.n_cap = n_cap; p.T = n_cap / BN; p.Hkv = Hkv;
+    // blocks that the rows can reach, wherever they begin
+    const int most = n_in < n_cap ? n_in : n_cap;
+    const long long tiles = old_lens ? (most + BN - 2LL) / BN + 1 : (n_new - 1) / BN - n_old / BN + 1;
+    if (tiles * 2 * Hkv * B > kMaxWorkgroups256) return VFA_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)tiles, (unsigned)(2 * Hkv), (unsigned)B);
+    (void)hipGetLastError();
+    with_d(d, [&](auto d_c) { kv8_append_kernel<decltype(d_c)::value><<<grid, 256, 0, (hipStream_t)stream>>>(p); });
+    return launched();
+}
+
+int vfa_kv8_read(const void* K8, const void* V8, const void* KS, const void* VS, void* K, void* V, int B, int Hkv, int n_cap, int n, int d,
+                 const int* seq_lens, int seq_len, void* stream) {
+    bool done;
+    const int rc = check_cache8(K8, V8, KS, VS, B, Hkv, n_cap, d, &done);
+    if (rc != VFA_OK || n < 0 || n > n_cap || !aligned4(seq_lens)) return rc != VFA_OK ? rc : VFA_ERR_INVALID_ARG;
+    if (done || n == 0) return VFA_OK;
+    if (!K || !V || !aligned16(K) || !aligned16(V)) return VFA_ERR_INVALID_ARG;
+    Kv8Read p{};
+    p.C[0] = (const uint8_t*)K8; p.C[1] = (const uint8_t*)V8; p.S[0] = (const uint8_t*)KS; p.S[1] = (const uint8_t*)VS;
+    p.Y[0] = (uint16_t*)K; p.Y[1] = (uint16_t*)V;
+    p.seq_lens = seq_lens; p.seq_len = seq_len; p.n = n; p.n_cap = n_cap; p.T = n_cap / BN; p.Hkv = Hkv;
+    const long long tiles = ceil_div(n, BN);
+    if (tiles * 2 * Hkv * B > kMaxWorkgroups256) return VFA_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)tiles, (unsigned)(2 * Hkv), (unsigned)B);
+    (void)hipGetLastError();
+    with_d(d, [&](auto d_c) { kv8_read_kernel<decltype(d_c)::value><<<grid, 256, 0, (hipStream_t)stream>>>(p); });
+    return launched();
+}
+
+int vfa_kv8_decode_splits(int B, int Hkv, int n_keys) {
+    if (B <= 0 || Hkv <= 0 || n_keys <= 0) return 1;
+    const long long heads = (long long)B * Hkv, all = ceil_div(n_keys, BN);
+    const long long n = (768 + heads - 1) / heads;
+    return (int)max(1LL, min(n, min((all + 3) / 4, 4096LL)));
+}
+
+size_t vfa_kv8_decode_workspace_bytes(int B, int Hq, int n_q, int d, int n_splits) {
+    if (B <= 0 || Hq <= 0 || n_q <= 0 || d <= 0 || n_splits <= 0) return 0;
+    const size_t bytes = (size_t)B * Hq * n_q * n_splits * (2 + (size_t)d) * sizeof(float);
+    return (bytes + 255) & ~(size_t)255;
+}
+
+int vfa_kv8_decode_fwd(const void* Q, const void* K8, const void* V8, const void* KS, const void* VS, void* O, float* LSE, int B, int Hq,
+                       int Hkv, int n_cap, int n_q, int d, const int* seq_lens, int n_keys, int n_splits, float softmax_scale,
+                       void* workspace, size_t workspace_bytes, void* stream) {
+    bool done;
+    const int rc = check_cache8(K8, V8, KS, VS, B, Hkv, n_cap, d, &done);
+    if (rc != VFA_OK) return rc;
+    if (Hq <= 0 || Hq % Hkv != 0 || n_q < 0 || n_splits < 1 || n_splits > 4096 || !isfinite(softmax_scale)) return VFA_ERR_INVALID_ARG;
+    if (!aligned4(seq_lens) || (!seq_lens && (n_keys < 0 || n_keys > n_cap))) return VFA_ERR_INVALID_ARG;
+    const long long rows = (long long)(Hq / Hkv) * n_q;
+    if (rows > 32) return VFA_ERR_UNSUPPORTED;
+    if (done || n_q == 0) return VFA_OK;
+    if (!Q || !O || !aligned16(Q) || !aligned16(O) || !aligned4(LSE)) return VFA_ERR_INVALID_ARG;
+    if ((long long)B * Hq * n_q > 0x7fffffffLL) return VFA_ERR_UNSUPPORTED;
+    if (n_splits > 1 && (!workspace || !aligned16(workspace) || workspace_bytes < vfa_kv8_decode_workspace_bytes(B, Hq, n_q, d, n_splits)))
+        return VFA_ERR_INVALID_ARG;
+    Kv8Decode P{};
+    DecodeParams& p = P.d;
+    P.K8 = (const uint8_t*)K8; P.V8 = (const uint8_t*)V8; P.KS = (const uint8_t*)KS; P.VS = (const uint8_t*)VS;
+    P.T = n_cap / BN; P.n_q = n_q;
+    p.Q = (const uint16_t*)Q; p.O = (uint16_t*)O; p.LSE = LSE;
+    p.B = B; p.Hq = Hq * n_q; p.Hkv = Hkv; p.n_cap = n_cap; p.n_keys = seq_lens ? n_cap : n_keys; p.seq_lens = seq_lens; p.n_splits = n_splits;
+    p.g = (int)rows;
+    p.c = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)d)) * kLog2e;
+    const size_t slots = (size_t)B * Hq * n_q * n_splits;
+    p.opart = (float*)workspace; p.pm = p.opart + slots * d; p.lpart = p.pm + slots;
+    hipStream_t s = (hipStream_t)stream;
+    const int n_cu = cu_count() > 0 ? cu_count() : 256;
+    (void)hipGetLastError();
+    const long long wgs = (long long)B * Hkv * n_splits;
+    if (wgs > kMaxWorkgroups256) return VFA_ERR_UNSUPPORTED;
+    const bool dealt = seq_lens && n_splits > 1 && (B <= 64 || (B <= DEAL_MAX_B && wgs <= 8LL * n_cu && ceil_div(n_cap, BN) > 2 * n_splits));
+    with_d(d, [&](auto d_c) {
+        constexpr int D = decltype(d_c)::value, W = 4;
+        auto launch = [&](auto rt_c) {
+            constexpr int RT = decltype(rt_c)::value;
+            const dim3 grid((unsigned)n_splits, (unsigned)B, (unsigned)Hkv);
+            if (!seq_lens) kv8_decode_kernel<D, RT, W, LENS_ONE><<<grid, 64 * W, 0, s>>>(P);
+            else if (dealt) kv8_decode_kernel<D, RT, W, LENS_DEALT><<<grid, 64 * W, 0, s>>>(P);
+            else kv8_decode_kernel<D, RT, W, LENS_FIXED><<<dim3((unsigned)n_splits, (unsigned)Hkv, (unsigned)B), 64 * W, 0, s>>>(P);
+        };
+        if (rows <= 16) launch(std::integral_constant<int, 1>{});
+        else launch(std::integral_constant<int, 2>{});
+        if (n_splits == 1) return;
+        const dim3 grid((unsigned)p.Hq, (unsigned)B);
+        if (dealt) decode_merge_kernel<D, true, true><<<grid, 256, 0, s>>>(p);
+        else decode_merge_kernel<D, false, true><<<grid, 256, 0, s>>>(p);
+    });
+    return launched();
+}
+
+}  // extern "C"

@@ -8,6 +8,7 @@
 #include "vfa.h"
 
 #include "common.hpp"
+#include "host.hpp"
 #include "attn_generic.hpp"
 #include "attn_pingpong.hpp"
 #include "attn_frozen.hpp"
@@ -23,12 +24,6 @@ namespace {
 
 // ---------------------------------------------------------------------------------------------
 // host side
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
-
-// Workgroups of 256 threads that one launch can have: of 2^32 work-items or more HIP runs a part, without an error
-constexpr long long kMaxWorkgroups256 = (1LL << 24) - 1;
-
 int check_common(const void* Q, const void* K, const void* V, void* O, const float* LSE, int B, int Hq, int Hkv,
                  int N, int d, int block_m, int block_n) {
     if (B < 0 || N < 0 || Hq <= 0 || Hkv <= 0 || d <= 0 || block_m <= 0 || block_n <= 0) return VFA_ERR_INVALID_ARG;
@@ -42,30 +37,6 @@ int check_common(const void* Q, const void* K, const void* V, void* O, const flo
     const long long wgs = (long long)B * Hq * ceil_div(N, block_m);
     if (wgs > 0x7fffffffLL || (long long)B * Hq * N > 0x7fffffffLL) return VFA_ERR_UNSUPPORTED;
     return VFA_OK;
-}
-
-// Host-side caches.  Everything the library remembers between calls is a per-device fact that any thread would
-// compute to the same value (a CU count, "this kernel's LDS limit has been raised", the address of the device
-// array below), held in atomics: two threads that race on a first call both do the lookup and store the same thing.
-constexpr int kMaxDevices = 64;
-
-int current_device() {
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return -1;
-    return dev;
-}
-
-// number of compute units of the current device (0 if the query fails), looked up once per device
-int cu_count() {
-    static std::atomic<int> cached[kMaxDevices];
-    const int dev = current_device();
-    if (dev < 0) return 0;
-    int n = cached[dev].load(std::memory_order_relaxed);
-    if (n == 0) {
-        if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) n = -1;
-        cached[dev].store(n, std::memory_order_relaxed);
-    }
-    return n > 0 ? n : 0;
 }
 
 // Opt the kernels that need more than 64 KiB of LDS in to it: all of them on the first attention call on a device, whatever call

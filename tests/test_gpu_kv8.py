@@ -1,0 +1,375 @@
+"""The 8-bit cache on the GPU: writing (codes and scales bit for bit), reading back (bit for bit), attention of one and more new tokens against
+64 bits, and a serving loop of all of them."""
+import math
+
+import pytest
+import torch
+
+import kv8_util as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def vfa():
+    assert torch.cuda.is_available(), "these tests need the GPU"
+    import paper_2604_12798_amd as pkg
+    pkg.lib()
+    return pkg
+
+
+def ints(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def rows(shape, seed, size=1.0):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(shape, generator=g) * size
+    x[..., : shape[-1] // 8] *= 7
+    return x.to(torch.bfloat16)
+
+
+def same_cache(cache, want, new):
+    """Tokens below `new` of each sequence, and the scales of their blocks."""
+    codes, exp = ref.unpack(cache)
+    for side in range(2):
+        for b, n in enumerate(new):
+            assert ref.same_codes(codes[side][b, :, :n], want.codes[side][b, :, :n]), (side, b)
+            t = -(-n // 64)
+            assert torch.equal(exp[side][b, :, :t], want.exp[side][b, :, :t]), (side, b)
+
+
+# ---- writing ---------------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 127, 300])
+def test_first_rows(vfa, d, n):
+    B, H, cap = 2, 3, 320
+    K, V = rows((B, H, n, d), n), rows((B, H, n, d), n + 1, 0.01)
+    cache = vfa.kv8_cache(B, H, cap, d)
+    for t in cache:
+        t.fill_(0x55)
+    vfa.kv8_append(K.cuda(), V.cuda(), cache, 0, n)
+    want = ref.Cache(B, H, cap, d)
+    want.append(K, V, [0] * B, [n] * B)
+    same_cache(cache, want, [n] * B)
+    codes, exp = ref.unpack(cache)
+    for side in range(2):  # what lies behind is as it was
+        assert (codes[side][:, :, n:] == 0x55).all() and (exp[side][:, :, -(-n // 64):] == 0x55 - 127).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_growing_with_larger_and_smaller_rows(vfa, d):
+    """Token by token and by more, over the ends of blocks; a row that needs a larger scale has the block coded again, and tokens behind a rewound
+    length are written anew."""
+    B, H, cap = 2, 2, 256
+    cache, want = vfa.kv8_cache(B, H, cap, d), ref.Cache(B, H, cap, d)
+    n, size = 0, [1, 1, 30, 0.01, 4, 1e4, 1, 1e-3, 1e5, 2, 2, 1e6, 1]
+    for i, step in enumerate((1, 1, 5, 50, 7, 1, 63, 64, 1, -20, 3, 17, 2)):
+        if step < 0:
+            n += step
+            continue
+        K, V = rows((B, H, step, d), 100 + i, size[i]), rows((B, H, step, d), 200 + i, size[-1 - i])
+        vfa.kv8_append(K.cuda(), V.cuda(), cache, n, n + step)
+        want.append(K, V, [n] * B, [n + step] * B)
+        n += step
+        same_cache(cache, want, [n] * B)
+
+
+def test_recoding_into_subnormals(vfa):
+    """Every code in a block whose scale grows by 2^0 to 2^40."""
+    for grow in (0, 1, 2, 3, 7, 9, 12, 18, 40):
+        codes = torch.arange(256, dtype=torch.uint8).repeat(32).reshape(1, 1, 64, 128)
+        want = ref.Cache(1, 1, 64, 128)
+        want.codes = [codes.clone(), codes.flip(2).contiguous()]
+        want.exp = [torch.full((1, 1, 1), -3, dtype=torch.int32) for _ in range(2)]
+        cache = ref.pack(want)
+        x = torch.full((1, 1, 1, 128), 448 * 2.0 ** (grow - 3)).to(torch.bfloat16)
+        vfa.kv8_append(x.cuda(), x.cuda(), cache, 63, 64)
+        want.append(x, x, [63], [64])
+        same_cache(cache, want, [64])
+
+
+def test_every_bf16(vfa):
+    """All finite values of bf16, 64 neighbours to a row, so that a block spans a few binades; then each alone with the largest of its block."""
+    bits = torch.arange(0, 65536, dtype=torch.int32).to(torch.int16).view(torch.bfloat16)
+    x = torch.where(bits.isfinite(), bits, torch.zeros_like(bits)).reshape(1, 1, 512, 128)
+    for y in (x, x.reshape(64, 8, 128).transpose(0, 1).reshape(1, 1, 512, 128).contiguous()):
+        cache, want = vfa.kv8_cache(1, 1, 512, 128), ref.Cache(1, 1, 512, 128)
+        vfa.kv8_append(y.cuda(), y.cuda(), cache, 0, 512)
+        want.append(y, y, [0], [512])
+        same_cache(cache, want, [512])
+
+
+def test_zeros_infinities_nan(vfa):
+    K = rows((1, 2, 130, 64), 5)
+    K[0, 0, 3, 7], K[0, 0, 4, 7], K[0, 0, 70, 0], K[0, 1, 129, 63] = math.inf, -math.inf, math.nan, math.nan
+    V = torch.zeros((1, 2, 130, 64), dtype=torch.bfloat16)
+    V[0, 0, :64] = math.inf
+    V[0, 1, :64] = math.nan
+    V[0, 1, 128] = -0.0
+    cache, want = vfa.kv8_cache(1, 2, 192, 64), ref.Cache(1, 2, 192, 64)
+    vfa.kv8_append(K.cuda(), V.cuda(), cache, 0, 130)
+    want.append(K, V, [0], [130])
+    same_cache(cache, want, [130])
+    assert int(cache[3][0, 0, 1]) == ref.E_MIN + 127
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_ragged_batch(vfa, d):
+    """Lengths of their own, among them empty, full, reversed, beyond the capacity and with more rows than were given."""
+    B, H, cap, n_in = 8, 2, 192, 70
+    old = [0, 0, 63, 64, 100, 150, -5, 192]
+    new = [0, 70, 64, 134, 60, 500, 3, 400]
+    o = [min(max(x, 0), cap) for x in old]
+    n = [min(min(y, cap), x + n_in) for x, y in zip(o, new)]
+    want = ref.random_cache(B, H, cap, d, 3)
+    cache = ref.pack(want)
+    K, V = rows((B, H, n_in, d), 1, 3), rows((B, H, n_in, d), 2, 0.1)
+    vfa.kv8_append(K.cuda(), V.cuda(), cache, ints(old), ints(new))
+    want.append(K, V, o, n)
+    same_cache(cache, want, [cap] * B)  # everything else is as it was
+
+
+def test_strides(vfa):
+    """Keys and values as slices of one projection, a head axis of stride zero, a batch run backwards through memory."""
+    B, H, n, d = 2, 3, 37, 128
+    x = rows((B, n, 2 * H, d), 8).cuda()
+    K, V = x[:, :, :H].transpose(1, 2), x[:, :, H:].transpose(1, 2)
+    one = x[:, :, :1].transpose(1, 2).expand(B, H, n, d)
+    for k, v in ((K, V), (one, K), (V.contiguous(), one)):
+        cache, want = vfa.kv8_cache(B, H, 64, d), ref.Cache(B, H, 64, d)
+        vfa.kv8_append(k, v, cache, 5, 5 + n)  # (rows 0 to 4 hold anything: only the new ones are looked at)
+        cache2 = vfa.kv8_cache(B, H, 64, d)
+        for a, c in zip(cache2, cache):
+            a.copy_(c)
+        vfa.kv8_append(k, v, cache2, 0, n)
+        want.append(k.cpu(), v.cpu(), [0] * B, [n] * B)
+        same_cache(cache2, want, [n] * B)
+
+
+# ---- reading back ----------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [1, 63, 64, 65, 192])
+def test_read(vfa, d, n):
+    B, H, cap = 4, 2, 192
+    want = ref.random_cache(B, H, cap, d, n)
+    want.codes[0][0, 0, 0, 0] = 127
+    lens = [n, 0, max(n - 1, 0), 500]
+    out = [torch.full((B, H, n, d), 9.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    got = vfa.kv8_read(ref.pack(want), n, seq_lens=ints(lens), out=out)
+    for x, v in zip(got, want.values()):
+        for b in range(B):
+            m = min(lens[b], n)
+            assert torch.equal(x[b, :, :m].cpu().nan_to_num(7.0), v[b, :, :m].to(torch.bfloat16).nan_to_num(7.0))
+            assert (x[b, :, m:] == 0).all()
+    again = vfa.kv8_read(ref.pack(want), n, seq_lens=n)
+    assert torch.equal(again[1][3], got[1][3])
+
+
+def test_read_extremes(vfa):
+    """Every code at the smallest, middle and largest exponents."""
+    want = ref.Cache(1, 1, 192, 128)
+    codes = torch.arange(256, dtype=torch.uint8).repeat(96).reshape(1, 1, 192, 128)
+    want.codes = [codes, codes.clone()]
+    want.exp = [torch.tensor([[[ref.E_MIN, -9, 120]]], dtype=torch.int32) for _ in range(2)]
+    for x, v in zip(vfa.kv8_read(ref.pack(want), 192), want.values()):
+        assert torch.equal(x.cpu().nan_to_num(7.0, 8.0, 9.0), v.to(torch.bfloat16).nan_to_num(7.0, 8.0, 9.0))
+
+
+# ---- attention -------------------------------------------------------------------------------------------------------------------
+
+def run_decode(vfa, B, Hq, Hkv, cap, d, n_q, lens, n_splits, seed=0, uniform=False, q_size=1.5, **kw):
+    c = ref.random_cache(B, Hkv, cap, d, seed)
+    q = rows((B, Hq, n_q, d), seed + 1, q_size / 4).cuda()
+    O = torch.full_like(q, math.nan)
+    L = torch.full(q.shape[:3], math.nan, device="cuda")
+    vfa.kv8_decode_fwd(q, ref.pack(c), lens[0] if uniform else ints(lens), n_splits=n_splits, out=O, lse=L, **kw)
+    want = ref.attend(q, c.values(), [min(max(n, 0), cap) for n in lens], **({"scale": kw["softmax_scale"]} if "softmax_scale" in kw else {}))
+    ref.check(O, L, want, (B, Hq, Hkv, cap, d, n_q, lens, n_splits))
+    return O, L
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("g", [1, 4, 7, 16, 17, 32])
+@pytest.mark.parametrize("n_splits", [1, 3, 24])
+def test_decode_lengths(vfa, d, g, n_splits):
+    lens = [0, 1, 63, 64, 65, 300, 512, 700, -3]
+    run_decode(vfa, len(lens), 2 * g, 2, 512, d, 1, lens, n_splits, seed=g)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("g,n_q", [(1, 2), (1, 32), (4, 4), (4, 5), (8, 4), (3, 10), (16, 2), (5, 6)])
+@pytest.mark.parametrize("n_splits", [1, 4])
+def test_several_new_tokens(vfa, d, g, n_q, n_splits):
+    """Among them sequences shorter than the number of new tokens, whose first ones see nothing, and new tokens on both sides of a block's end."""
+    lens = [0, 1, n_q - 1, n_q, 64, 65, 64 + n_q // 2, 200]
+    run_decode(vfa, len(lens), 2 * g, 2, 256, d, n_q, lens, n_splits, seed=n_q)
+
+
+@pytest.mark.parametrize("n", [0, 1, 64, 1000])
+@pytest.mark.parametrize("n_splits", [None, 1, 5])
+def test_one_length_for_all(vfa, n, n_splits):
+    run_decode(vfa, 2, 8, 2, 1024, 128, 1, [n, n], n_splits, uniform=True, seed=n)
+    run_decode(vfa, 2, 8, 2, 1024, 64, 3, [n, n], n_splits, uniform=True, seed=n)
+
+
+@pytest.mark.parametrize("B,n_splits", [(70, 2), (256, 3), (300, 2), (300, 1)])
+def test_many_sequences(vfa, B, n_splits):
+    """Batches whose ranges are dealt out, and batches above that."""
+    run_decode(vfa, B, 4, 1, 320, 64, 1, [(37 * b) % 321 for b in range(B)], n_splits, seed=B)
+
+
+def test_scale_and_large_scores(vfa):
+    run_decode(vfa, 2, 4, 2, 256, 128, 1, [256, 100], 2, softmax_scale=0.5)
+    run_decode(vfa, 2, 4, 2, 256, 128, 2, [256, 100], 2, q_size=20.0)
+
+
+def test_nothing_behind_the_end_is_seen(vfa):
+    """NaN codes and scales of any kind behind a sequence's end, in its last block and beyond."""
+    B, H, cap, d = 3, 2, 256, 128
+    lens = [1, 70, 190]
+    c = ref.random_cache(B, H, cap, d, 1)
+    q = rows((B, 8, 2, d), 2, 0.4).cuda()
+    clean = vfa.kv8_decode_fwd(q, ref.pack(c), ints(lens), n_splits=2)
+    for side in range(2):
+        for b, n in enumerate(lens):
+            c.codes[side][b, :, n:] = 0x7f
+            c.exp[side][b, :, -(-n // 64):] = 128
+    dirty = vfa.kv8_decode_fwd(q, ref.pack(c), ints(lens), n_splits=2)
+    assert torch.equal(clean[0], dirty[0]) and torch.equal(clean[1], dirty[1])
+
+
+@pytest.mark.parametrize("d,g", [(64, 2), (128, 6)])
+def test_nan_of_a_draft_reaches_those_who_see_it(vfa, d, g):
+    """Keys and values that are NaN from the second and third of four new tokens: the tokens before them are clean."""
+    B, H, cap, n_q = 2, 1, 192, 4
+    lens = [66, 140]
+    for side in range(2):
+        c = ref.random_cache(B, H, cap, d, 7)
+        for b, n in enumerate(lens):
+            c.codes[side][b, :, n - 3, 5] = 0x7f
+            c.codes[side][b, :, n - 2, d - 1] = 0xff
+        q = rows((B, g, n_q, d), 8, 0.4).cuda()
+        for ns in (1, 2):
+            O, L = vfa.kv8_decode_fwd(q, ref.pack(c), ints(lens), n_splits=ns)
+            want = ref.attend(q, c.values(), lens)
+            assert not want[0][:, :, 0].isnan().any() and want[0][:, :, 1:].isnan().any()
+            ref.check(O, L, want, (side, ns))
+
+
+def test_offsets_past_32_bits(vfa):
+    """Sequences that begin beyond 2^31 bytes of codes."""
+    B, H, cap, d = 3, 8, 1 << 20, 128
+    free, _ = torch.cuda.mem_get_info()
+    if free < 12 << 30:
+        pytest.skip("needs 12 GiB")
+    cache = vfa.kv8_cache(B, H, cap, d)
+    n, far = 100, cap - 130
+    K, V = rows((B, H, n, d), 1), rows((B, H, n, d), 2)
+    vfa.kv8_append(K.cuda(), V.cuda(), cache, 0, n)
+    small = vfa.kv8_cache(B, H, 128, d)
+    vfa.kv8_append(K.cuda(), V.cuda(), small, 0, n)
+    q = rows((B, 16, 1, d), 3).cuda()
+    a, b = vfa.kv8_decode_fwd(q, cache, ints([n] * B), n_splits=2), vfa.kv8_decode_fwd(q, small, ints([n] * B), n_splits=2)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    vfa.kv8_append(K.cuda(), V.cuda(), cache, ints([far] * B), ints([far + n] * B))
+    t0 = far // 64
+    want = ref.Cache(B, H, 256, d)
+    want.append(K, V, [far % 64] * B, [far % 64 + n] * B)
+    part = tuple(t[:, :, t0: t0 + 3].contiguous() for t in cache)
+    codes, _ = ref.unpack(part)
+    lo = 64 - far % 64  # the first block's old rows hold anything, and its scale with them
+    for side in range(2):
+        assert ref.same_codes(codes[side][:, :, 64: far % 64 + n], want.codes[side][:, :, 64: far % 64 + n]), lo
+    del cache
+
+
+def test_same_bits_again_and_on_another_stream(vfa):
+    B, Hq, H, cap, d = 4, 8, 2, 2048, 128
+    c = ref.pack(ref.random_cache(B, H, cap, d, 4))
+    q, lens = rows((B, Hq, 2, d), 5).cuda(), ints([2048, 1, 900, 65])
+    first = vfa.kv8_decode_fwd(q, c, lens)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        second = vfa.kv8_decode_fwd(q, c, lens)
+    third = vfa.kv8_decode_fwd(q, c, lens, stream=s)
+    s.synchronize()
+    for x in (second, third):
+        assert torch.equal(first[0], x[0]) and torch.equal(first[1], x[1])
+
+
+# ---- together --------------------------------------------------------------------------------------------------------------------
+
+def table(n, rot):
+    a = torch.arange(n, dtype=torch.float64)[:, None] * 10000.0 ** (-torch.arange(0, rot, 2, dtype=torch.float64) / rot)
+    return torch.cat((a.cos(), a.sin()), 1).float().cuda()
+
+
+def test_serving_loop(vfa):
+    """A ragged batch of prompts (normed, rotated, prefilled in bf16, written to the cache), then steps of one and of three tokens, each against 64 bits
+    over what the cache stands for; the prompts' last tokens come out of both attention paths alike."""
+    B, Hq, H, d, cap = 2, 8, 2, 128, 256
+    cs, w = table(cap, d), (1 + 0.1 * rows((2, d), 1)).cuda()
+    kw = dict(q_weight=w[0], k_weight=w[1], cos_sin=cs)
+    cache, want = vfa.kv8_cache(B, H, cap, d), ref.Cache(B, H, cap, d)
+    lens = [97, 64]
+    x = rows((B, 97, Hq + 2 * H, d), 2).cuda()
+    Q, K, V = vfa.qk_norm_rope_fwd(x[:, :, :Hq], x[:, :, Hq: Hq + H], x[:, :, Hq + H:], **kw)
+    O, L = vfa.vfa_attn_fwd(Q, K, V)
+    vfa.kv8_append(K, V, cache, ints([0, 0]), ints(lens))
+    want.append(K.cpu(), V.cpu(), [0, 0], lens)
+    last = torch.stack([Q[b, :, n - 2: n] for b, n in enumerate(lens)])
+    O8, L8 = vfa.kv8_decode_fwd(last, cache, ints(lens))
+    ref.check(O8, L8, ref.attend(last, want.values(), lens))
+    for b, n in enumerate(lens):  # (8-bit keys and values: scores off by a few hundredths, values by 2^-4 at most)
+        assert (O8[b].float() - O[b, :, n - 2: n].float()).abs().mean() < 0.05 * O[b, :, n - 2: n].float().abs().mean() + 0.02
+    for i, step in enumerate((1, 3, 1, 1, 3)):
+        x = rows((B, step, Hq + 2 * H, d), 10 + i, 1 + i).cuda()
+        Q, K, V = vfa.qk_norm_rope_fwd(x[:, :, :Hq], x[:, :, Hq: Hq + H], x[:, :, Hq + H:], first_pos=ints(lens), **kw)
+        new = [n + step for n in lens]
+        vfa.kv8_append(K, V, cache, ints(lens), ints(new))
+        want.append(K.cpu(), V.cpu(), lens, new)
+        O, L = vfa.kv8_decode_fwd(Q, cache, ints(new))
+        same_cache(cache, want, new)
+        ref.check(O, L, ref.attend(Q, want.values(), new), i)
+        lens = new if step == 1 else [n + 1 for n in lens]  # (two of three drafts are refused)
+
+
+def test_step_in_a_graph(vfa):
+    """A whole step captured once; lengths and inputs change between the replays, with eager steps on a cache of its own beside them."""
+    B, Hq, H, d, cap = 3, 8, 2, 64, 256
+    cs = table(cap, d)
+
+    def step(x, cache, lens, new, ws, out, lse):
+        Q, K, V = vfa.qk_norm_rope_fwd(x[:, :, :Hq], x[:, :, Hq: Hq + H], x[:, :, Hq + H:], norm=False, cos_sin=cs, first_pos=lens)
+        vfa.kv8_append(K, V, cache, lens, new)
+        vfa.kv8_decode_fwd(Q, cache, new, n_splits=4, workspace=ws, out=out, lse=lse)
+
+    caches = [vfa.kv8_cache(B, H, cap, d) for _ in range(2)]
+    for c in caches:
+        for t in c:
+            t.zero_()
+    lens, new = ints([0, 60, 126]), ints([1, 61, 127])
+    x = rows((B, 1, Hq + 2 * H, d), 0).cuda()
+    outs = [torch.empty((B, Hq, 1, d), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    lses = [torch.empty((B, Hq, 1), device="cuda") for _ in range(2)]
+    spaces = [torch.empty(vfa.kv8_decode_workspace_bytes(B, Hq, 1, d, 4), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    step(x, caches[1], lens, new, spaces[1], outs[1], lses[1])  # (loads the kernels)
+    for t in caches[1]:
+        t.zero_()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(x, caches[0], lens, new, spaces[0], outs[0], lses[0])
+    for i in range(6):
+        x.copy_(rows(x.shape, 20 + i, 1 + 5 * i).cuda())
+        graph.replay()
+        step(x, caches[1], lens, new, spaces[1], outs[1], lses[1])
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], outs[1]) and torch.equal(lses[0], lses[1]), i
+        assert all(torch.equal(a, b) for a, b in zip(*caches)), i
+        lens += 1
+        new += 1
