@@ -454,30 +454,37 @@ def mxfp4_attn_fwd(Q4, QS, K4, KS, Vt8, *, descale_v, frozen=True, block_m=128, 
     return O, L, ws
 
 
-def _lengths(x, B, device, what):
+_empty = _f32 = _u8 = _tensor = None
+
+
+def _serving(device):
+    """The tensors of a call lie on the GPU `device`: it has to be the current one, whose stream is used."""
+    if device != _current_device():
+        raise ValueError(f"tensors must be on the current GPU ({_current_device()}), not on {device}")
+
+
+def _ns():
+    """_n(), and what the wrappers of the serving operators use of torch on every call."""
+    global _empty, _f32, _u8, _tensor, _current_device, _current_stream
+    if _empty is None:
+        import torch
+        _empty, _f32, _u8, _tensor = torch.empty, torch.float32, torch.uint8, torch.Tensor
+        _current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+    return _native or _n()
+
+
+def _lengths(x, n, B, device, what):
     """(device array or None, whole number) of lengths that are one for all or an int32 tensor of B entries."""
-    import torch
-    if not isinstance(x, torch.Tensor):
+    if not isinstance(x, _tensor):
         return None, int(x)
-    if x.dtype != _i32 or x.device != device or x.dim() != 1 or x.shape[0] != B or not x.is_contiguous():
-        raise ValueError(f"{what} must be a whole number or a contiguous int32 tensor of {B} entries on {device}")
+    if not n.check_tensor(x, _i32, device, B):
+        raise ValueError(f"{what} must be a whole number or a contiguous int32 tensor of {B} entries on the same GPU")
     return x, 0
 
 
-def _on_device(*tensors):
-    """All of the tensors that are there lie on the current GPU."""
-    import torch
-    _n()
-    here = torch.device("cuda", torch.cuda.current_device()) if torch.cuda.is_available() else None
-    for t in tensors:
-        if t is not None and t.device != here:
-            raise ValueError(f"tensors must be on the current GPU ({here}), not on {t.device}")
-    return here
-
-
-def _bf16_rows(x, dims, what):
-    if x.dtype != _bf16 or x.dim() != dims or x.stride(-1) != 1:
-        raise ValueError(f"{what} must be a bf16 tensor of {dims} dimensions whose last one is contiguous")
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
 
 
 def qk_norm_rope_fwd(q, k, v=None, *, norm=True, q_weight=None, k_weight=None, eps=1e-6, cos_sin=None, interleaved=False, first_pos=0,
@@ -486,37 +493,27 @@ def qk_norm_rope_fwd(q, k, v=None, *, norm=True, q_weight=None, k_weight=None, e
     K, V [B, Hkv, N, d] as the attention calls take them: queries and keys normed over each head (norm=True; weights [d] or None) and
     rotated by position (cos_sin [n_pos, rot] fp32: cosines, then sines; None: no rotation).  first_pos: position of token 0, a
     number or an int32 tensor of B entries.  out: (Q, K, V) to write to."""
-    import torch
-    dev = _on_device(q, k, v, q_weight, k_weight, cos_sin)
-    _bf16_rows(q, 4, "q"), _bf16_rows(k, 4, "k")
-    B, N, Hq, d = q.shape
-    Hkv = k.shape[2]
-    if k.shape != (B, N, Hkv, d) or (v is not None and v.shape != k.shape):
-        raise ValueError("k, v must be [B, N, Hkv, d] matching q [B, N, Hq, d]")
-    if v is not None:
-        _bf16_rows(v, 4, "v")
+    n = _ns()
+    dev, B, N, Hq, Hkv, d, *strides = n.check_norm_rope(q, k, v, _bf16)
+    _serving(dev)
     for w in (q_weight, k_weight):
-        if w is not None and (w.dtype != _bf16 or w.shape != (d,) or not w.is_contiguous()):
-            raise ValueError("weights must be contiguous bf16 tensors of d entries")
+        _need(w is None or n.check_tensor(w, _bf16, dev, d), "weights must be contiguous bf16 tensors of d entries on the same GPU")
     n_pos = rot = 0
     if cos_sin is not None:
-        if cos_sin.dtype != torch.float32 or cos_sin.dim() != 2 or not cos_sin.is_contiguous():
-            raise ValueError("cos_sin must be a contiguous fp32 tensor [n_pos, rot]")
+        _need(cos_sin.dim() == 2, "cos_sin must be a contiguous fp32 tensor [n_pos, rot] on the same GPU")
         n_pos, rot = cos_sin.shape
-    at, first = _lengths(first_pos, B, dev, "first_pos")
-    shapes = ((B, Hq, N, d), (B, Hkv, N, d), (B, Hkv, N, d))
+        _need(n.check_tensor(cos_sin, _f32, dev, n_pos, rot), "cos_sin must be a contiguous fp32 tensor [n_pos, rot] on the same GPU")
+    at, first = _lengths(first_pos, n, B, dev, "first_pos")
     if out is None:
-        Q, K = (torch.empty(s, dtype=_bf16, device=dev) for s in shapes[:2])
-        V = None if v is None else torch.empty(shapes[2], dtype=_bf16, device=dev)
+        Q, K = q.new_empty((B, Hq, N, d)), q.new_empty((B, Hkv, N, d))
+        V = None if v is None else q.new_empty((B, Hkv, N, d))
     else:
         Q, K, V = out
-        _on_device(Q, K, V)
-        for t, s in zip((Q, K, V), shapes):
-            if t is not None and (t.dtype != _bf16 or t.shape != s or not t.is_contiguous()):
-                raise ValueError("out must be contiguous bf16 tensors [B, Hq, N, d], [B, Hkv, N, d], [B, Hkv, N, d]")
-    rc = _native.vfa_qk_norm_rope_fwd_t(q, k, v, Q, K, V, B, N, Hq, Hkv, d, *q.stride()[:3], *k.stride()[:3],
-                                        *((0, 0, 0) if v is None else v.stride()[:3]), int(bool(norm)), q_weight, k_weight, float(eps),
-                                        cos_sin, n_pos, rot, int(bool(interleaved)), at, first, _stream(stream))
+        _need(n.check_tensor(Q, _bf16, dev, B, Hq, N, d) and n.check_tensor(K, _bf16, dev, B, Hkv, N, d)
+              and (V is None or n.check_tensor(V, _bf16, dev, B, Hkv, N, d)),
+              "out must be contiguous bf16 tensors [B, Hq, N, d], [B, Hkv, N, d], [B, Hkv, N, d] on the same GPU")
+    rc = n.vfa_qk_norm_rope_fwd_t(q, k, v, Q, K, V, B, N, Hq, Hkv, d, *strides, int(bool(norm)), q_weight, k_weight, float(eps),
+                                  cos_sin, n_pos, rot, int(bool(interleaved)), at, first, _stream(stream))
     if rc != 0:
         raise VfaError(rc, "vfa_qk_norm_rope_fwd")
     return Q, K, V
@@ -524,40 +521,24 @@ def qk_norm_rope_fwd(q, k, v=None, *, norm=True, q_weight=None, k_weight=None, e
 
 def kv8_cache(B: int, Hkv: int, n_cap: int, d: int, device=None):
     """An 8-bit cache for B sequences of up to n_cap tokens (rounded up to whole blocks of 64): the tensors (K8, V8, KS, VS) of vfa.h, not
-    initialised."""
+    initialised.  device: the current GPU if not given."""
     import torch
-    dev = torch.device("cuda", torch.cuda.current_device()) if device is None else device
+    dev = "cuda" if device is None else device
     T = -(-n_cap // 64)
     shapes = ((B, Hkv, T, d // 64, 64, 64), (B, Hkv, T, d, 64), (B, Hkv, T), (B, Hkv, T))
     return tuple(torch.empty(s, dtype=torch.uint8, device=dev) for s in shapes)
 
 
-def _cache8(cache):
-    """B, Hkv, n_cap, d of a cache, and its device."""
-    import torch
-    K8, V8, KS, VS = cache
-    dev = _on_device(K8, V8, KS, VS)
-    if any(t.dtype != torch.uint8 or not t.is_contiguous() for t in cache) or K8.dim() != 6:
-        raise ValueError("a cache is four contiguous uint8 tensors (see kv8_cache)")
-    B, Hkv, T, s = K8.shape[:4]
-    if K8.shape[4:] != (64, 64) or V8.shape != (B, Hkv, T, 64 * s, 64) or KS.shape != (B, Hkv, T) or VS.shape != (B, Hkv, T):
-        raise ValueError("a cache is K8 [B, Hkv, T, d / 64, 64, 64], V8 [B, Hkv, T, d, 64], KS and VS [B, Hkv, T]")
-    return B, Hkv, 64 * T, 64 * s, dev
-
-
 def kv8_append(K, V, cache, old_lens, new_lens, stream=None):
     """Writes rows of K, V [B, Hkv, n_in, d] (bf16, any strides) into the cache, in place, as tokens old_lens <= n < new_lens of each
     sequence (numbers, or int32 tensors of B entries, both alike)."""
-    B, Hkv, n_cap, d, dev = _cache8(cache)
-    _on_device(K, V)
-    _bf16_rows(K, 4, "K"), _bf16_rows(V, 4, "V")
-    n_in = K.shape[2]
-    if K.shape != (B, Hkv, n_in, d) or V.shape != K.shape:
-        raise ValueError("K, V must be [B, Hkv, n_in, d] matching the cache")
-    (o, n_old), (n, n_new) = _lengths(old_lens, B, dev, "old_lens"), _lengths(new_lens, B, dev, "new_lens")
-    if (o is None) != (n is None):
-        raise ValueError("old_lens and new_lens must both be numbers or both be tensors")
-    rc = _native.vfa_kv8_append_t(K, V, *cache, B, Hkv, n_cap, n_in, d, *K.stride()[:3], *V.stride()[:3], o, n, n_old, n_new, _stream(stream))
+    n = _ns()
+    K8, V8, KS, VS = cache
+    dev, B, Hkv, n_cap, n_in, d, *strides = n.check_kv8_append(K, V, K8, V8, KS, VS, _bf16, _u8)
+    _serving(dev)
+    (o, n_old), (m, n_new) = _lengths(old_lens, n, B, dev, "old_lens"), _lengths(new_lens, n, B, dev, "new_lens")
+    _need((o is None) == (m is None), "old_lens and new_lens must both be numbers or both be tensors")
+    rc = n.vfa_kv8_append_t(K, V, K8, V8, KS, VS, B, Hkv, n_cap, n_in, d, *strides, o, m, n_old, n_new, _stream(stream))
     if rc != 0:
         raise VfaError(rc, "vfa_kv8_append")
     return cache
@@ -566,16 +547,20 @@ def kv8_append(K, V, cache, old_lens, new_lens, stream=None):
 def kv8_read(cache, n: int, *, seq_lens=None, out=None, stream=None):
     """The first n tokens of every sequence in bf16: K, V [B, Hkv, n, d], zeros at and behind seq_lens (a number or an int32 tensor of B
     entries; None: n)."""
-    import torch
-    B, Hkv, n_cap, d, dev = _cache8(cache)
-    lens, length = _lengths(n if seq_lens is None else seq_lens, B, dev, "seq_lens")
-    shape = (B, Hkv, max(int(n), 0), d)
-    K, V = (torch.empty(shape, dtype=_bf16, device=dev) for _ in range(2)) if out is None else out
-    if out is not None:
-        _on_device(K, V)
-        if any(t.dtype != _bf16 or t.shape != shape or not t.is_contiguous() for t in (K, V)):
-            raise ValueError("out must be two contiguous bf16 tensors [B, Hkv, n, d]")
-    rc = _native.vfa_kv8_read_t(*cache, K, V, B, Hkv, n_cap, int(n), d, lens, length, _stream(stream))
+    nat = _ns()
+    K8, V8, KS, VS = cache
+    dev, B, Hkv, n_cap, d = nat.check_cache8(K8, V8, KS, VS, _u8)
+    _serving(dev)
+    n = int(n)
+    _need(0 <= n <= n_cap, f"n must be between 0 and the cache's {n_cap} tokens")
+    lens, length = _lengths(n if seq_lens is None else seq_lens, nat, B, dev, "seq_lens")
+    if out is None:
+        K, V = K8.new_empty((B, Hkv, n, d), dtype=_bf16), K8.new_empty((B, Hkv, n, d), dtype=_bf16)
+    else:
+        K, V = out
+        _need(nat.check_tensor(K, _bf16, dev, B, Hkv, n, d) and nat.check_tensor(V, _bf16, dev, B, Hkv, n, d),
+              "out must be two contiguous bf16 tensors [B, Hkv, n, d] on the same GPU")
+    rc = nat.vfa_kv8_read_t(K8, V8, KS, VS, K, V, B, Hkv, n_cap, n, d, lens, length, _stream(stream))
     if rc != 0:
         raise VfaError(rc, "vfa_kv8_read")
     return K, V
@@ -591,28 +576,32 @@ def kv8_decode_splits(B: int, Hkv: int, n_keys: int) -> int:
 
 def kv8_decode_fwd(q, cache, seq_lens, *, n_splits=None, softmax_scale=0.0, workspace=None, out=None, lse=None, want_lse=True, stream=None):
     """Attention of each sequence's newest tokens, q [B, Hq, n_q, d] (or [B, Hq, d] for one), over the cache that holds them already;
-    seq_lens: a number or an int32 tensor of B entries.  n_splits: key ranges (None: vfa_kv8_decode_splits of the cache's capacity)."""
-    import torch
-    B, Hkv, n_cap, d, dev = _cache8(cache)
-    _on_device(q)
-    if q.dtype != _bf16 or not q.is_contiguous() or q.dim() not in (3, 4) or q.shape[0] != B or q.shape[-1] != d:
-        raise ValueError("q must be a contiguous bf16 tensor [B, Hq, n_q, d] or [B, Hq, d] matching the cache")
-    Hq, n_q = q.shape[1], q.shape[2] if q.dim() == 4 else 1
-    lens, n_keys = _lengths(seq_lens, B, dev, "seq_lens")
-    if n_splits is None:
-        n_splits = _native.vfa_kv8_decode_splits(B, Hkv, n_cap if lens is not None else n_keys)
-    O = torch.empty_like(q) if out is None else out
-    L = torch.empty(q.shape[:-1], dtype=torch.float32, device=dev) if lse is None and want_lse else lse
-    _on_device(O, L, workspace)
-    if O.dtype != _bf16 or O.shape != q.shape or not O.is_contiguous():
-        raise ValueError("out must be a contiguous bf16 tensor of q's shape")
-    if L is not None and (L.dtype != torch.float32 or L.shape != q.shape[:-1] or not L.is_contiguous()):
-        raise ValueError("lse must be a contiguous fp32 tensor of q's shape without d")
-    ws = workspace
-    if ws is None and n_splits > 1:
-        ws = torch.empty(kv8_decode_workspace_bytes(B, Hq, n_q, d, n_splits), dtype=torch.uint8, device=dev)
-    rc = _native.vfa_kv8_decode_fwd_t(q, *cache, O, L, B, Hq, Hkv, n_cap, n_q, d, lens, n_keys, int(n_splits), float(softmax_scale), ws,
-                                      0 if ws is None else _native.bytes_of(ws), _stream(stream))
+    seq_lens: a number or an int32 tensor of B entries.  n_splits: key ranges (None: vfa_kv8_decode_splits, of the cache's capacity where the
+    lengths are on the GPU).  A workspace of kv8_decode_workspace_bytes is for calls that must not allocate."""
+    n = _ns()
+    K8, V8, KS, VS = cache
+    dev, B, Hq, Hkv, n_cap, n_q, d = n.check_kv8_decode(q, K8, V8, KS, VS, _bf16, _u8)
+    _serving(dev)
+    lens, n_keys = _lengths(seq_lens, n, B, dev, "seq_lens")
+    n_splits = n.vfa_kv8_decode_splits(B, Hkv, n_cap if lens is not None else n_keys) if n_splits is None else int(n_splits)
+    if out is None:
+        out = q.new_empty(q.shape)
+    else:
+        _need(n.check_tensor(out, _bf16, dev, *q.shape), "out must be a contiguous bf16 tensor of q's shape on the same GPU")
+    if lse is not None:
+        _need(n.check_tensor(lse, _f32, dev, *q.shape[:-1]), "lse must be a contiguous fp32 tensor of q's shape without d on the same GPU")
+    elif want_lse:
+        lse = q.new_empty(q.shape[:-1], dtype=_f32)
+    ws_bytes = 0
+    if n_splits > 1:
+        if workspace is None:
+            ws_bytes = n.vfa_kv8_decode_workspace_bytes(B, Hq, n_q, d, n_splits)
+            workspace = K8.new_empty((ws_bytes,))
+        else:
+            _need(workspace.get_device() == dev and workspace.is_contiguous(), "the workspace must be a contiguous tensor on the same GPU")
+            ws_bytes = n.bytes_of(workspace)
+    rc = n.vfa_kv8_decode_fwd_t(q, K8, V8, KS, VS, out, lse, B, Hq, Hkv, n_cap, n_q, d, lens, n_keys, n_splits, float(softmax_scale),
+                                workspace, ws_bytes, _stream(stream))
     if rc != 0:
         raise VfaError(rc, "vfa_kv8_decode_fwd")
-    return O, L
+    return out, lse

@@ -34,12 +34,13 @@ bool convert(PyObject* o, float& v) {
 
 // Attribute and method names, made once when the module is loaded.
 struct Names {
-    PyObject *data_ptr, *is_cuda, *dtype, *is_contiguous, *dim, *shape, *numel, *element_size;
+    PyObject *data_ptr, *is_cuda, *dtype, *is_contiguous, *dim, *shape, *numel, *element_size, *get_device, *stride;
     bool make() {
         return (data_ptr = PyUnicode_InternFromString("data_ptr")) && (is_cuda = PyUnicode_InternFromString("is_cuda")) &&
                (dtype = PyUnicode_InternFromString("dtype")) && (is_contiguous = PyUnicode_InternFromString("is_contiguous")) &&
                (dim = PyUnicode_InternFromString("dim")) && (shape = PyUnicode_InternFromString("shape")) &&
-               (numel = PyUnicode_InternFromString("numel")) && (element_size = PyUnicode_InternFromString("element_size"));
+               (numel = PyUnicode_InternFromString("numel")) && (element_size = PyUnicode_InternFromString("element_size")) &&
+               (get_device = PyUnicode_InternFromString("get_device")) && (stride = PyUnicode_InternFromString("stride"));
     }
 } names;
 
@@ -173,6 +174,132 @@ PyObject* bytes_of(PyObject*, PyObject* t) {
     return e.o ? PyNumber_Multiply(n.o, e.o) : nullptr;
 }
 
+// The serving operators' tensors: 1, 0, or -1 with an error set, as above.  All of them lie on one GPU, whose index goes to `device` (-1 at first).
+int on_device(PyObject* t, PyObject* dtype, long& device) {
+    int ok = truth(attribute(t, names.is_cuda));
+    if (ok != 1) return ok;
+    {
+        const Ref d = attribute(t, names.dtype);
+        ok = d.o ? PyObject_RichCompareBool(d.o, dtype, Py_EQ) : -1;
+        if (ok != 1) return ok;
+    }
+    const Ref i = method(t, names.get_device);
+    const long at = i.o ? PyLong_AsLong(i.o) : -1;
+    if (at == -1 && PyErr_Occurred()) return -1;
+    if (device < 0) device = at;
+    return at == device;
+}
+// ... of `n` dimensions, contiguous; the shape goes to v
+int whole_tensor(PyObject* t, PyObject* dtype, long& device, Py_ssize_t n, long long* v) {
+    int ok = on_device(t, dtype, device);
+    if (ok == 1) ok = truth(method(t, names.is_contiguous));
+    if (ok != 1) return ok;
+    const Ref s = attribute(t, names.shape);
+    if (!s.o) return -1;
+    const Py_ssize_t have = PySequence_Size(s.o);
+    if (have != n) return have < 0 ? -1 : 0;
+    return entries(s, n, true, v) ? 1 : -1;
+}
+// ... of four dimensions, the last one contiguous; shape and strides
+int rows_tensor(PyObject* t, PyObject* dtype, long& device, long long* v, long long* st) {
+    const int ok = on_device(t, dtype, device);
+    if (ok != 1) return ok;
+    const Ref s = attribute(t, names.shape), r = method(t, names.stride);
+    if (!s.o || !r.o) return -1;
+    const Py_ssize_t have = PySequence_Size(s.o);
+    if (have != 4) return have < 0 ? -1 : 0;
+    if (!entries(s, 4, true, v) || !entries(r, 4, true, st)) return -1;
+    return st[3] == 1 || v[3] <= 1;
+}
+PyObject* refused(int ok, const char* what) {
+    if (ok == 0) PyErr_SetString(PyExc_ValueError, what);
+    return nullptr;
+}
+// K8, V8, KS, VS of a cache; (B, Hkv, T, d / 64) go to v
+int cache8(PyObject* const* c, PyObject* uint8, long& device, long long* v) {
+    long long k[6], x[5], a[3], b[3];
+    int ok = whole_tensor(c[0], uint8, device, 6, k);
+    if (ok == 1) ok = whole_tensor(c[1], uint8, device, 5, x);
+    if (ok == 1) ok = whole_tensor(c[2], uint8, device, 3, a);
+    if (ok == 1) ok = whole_tensor(c[3], uint8, device, 3, b);
+    if (ok != 1) return ok;
+    for (int i = 0; i < 3; ++i)
+        if (x[i] != k[i] || a[i] != k[i] || b[i] != k[i]) return 0;
+    for (int i = 0; i < 4; ++i) v[i] = k[i];
+    return k[4] == 64 && k[5] == 64 && x[3] == 64 * k[3] && x[4] == 64;
+}
+const char kCache8[] = "a cache is four contiguous uint8 tensors on one GPU: K8 [B, Hkv, T, d / 64, 64, 64], V8 [B, Hkv, T, d, 64], KS and VS [B, Hkv, T]";
+
+// check_cache8(K8, V8, KS, VS, uint8) -> (device, B, Hkv, n_cap, d)
+PyObject* check_cache8(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 5) return PyErr_Format(PyExc_TypeError, "expected 5 arguments, got %zd", n);
+    long device = -1;
+    long long c[4];
+    const int ok = cache8(args, args[4], device, c);
+    if (ok != 1) return refused(ok, kCache8);
+    return Py_BuildValue("(lLLLL)", device, c[0], c[1], 64 * c[2], 64 * c[3]);
+}
+// check_kv8_append(K, V, K8, V8, KS, VS, bfloat16, uint8) -> (device, B, Hkv, n_cap, n_in, d, strides of K, strides of V)
+PyObject* check_kv8_append(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 8) return PyErr_Format(PyExc_TypeError, "expected 8 arguments, got %zd", n);
+    long device = -1;
+    long long c[4], k[4], v[4], ks[4], vs[4];
+    int ok = cache8(args + 2, args[7], device, c);
+    if (ok != 1) return refused(ok, kCache8);
+    ok = rows_tensor(args[0], args[6], device, k, ks);
+    if (ok == 1) ok = rows_tensor(args[1], args[6], device, v, vs);
+    if (ok == 1) ok = k[0] == c[0] && k[1] == c[1] && k[3] == 64 * c[3] && v[0] == k[0] && v[1] == k[1] && v[2] == k[2] && v[3] == k[3];
+    if (ok != 1) return refused(ok, "K, V must be bf16 tensors [B, Hkv, n_in, d] matching the cache and on its GPU, their last dimension contiguous");
+    return Py_BuildValue("(lLLLLLLLLLLL)", device, c[0], c[1], 64 * c[2], k[2], 64 * c[3], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2]);
+}
+// check_kv8_decode(q, K8, V8, KS, VS, bfloat16, uint8) -> (device, B, Hq, Hkv, n_cap, n_q, d)
+PyObject* check_kv8_decode(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 7) return PyErr_Format(PyExc_TypeError, "expected 7 arguments, got %zd", n);
+    long device = -1;
+    long long c[4], q[4] = {0, 0, 1, 0};
+    int ok = cache8(args + 1, args[6], device, c);
+    if (ok != 1) return refused(ok, kCache8);
+    const Ref dims = method(args[0], names.dim);
+    const long nd = dims.o ? PyLong_AsLong(dims.o) : -1;
+    if (nd == -1 && PyErr_Occurred()) return nullptr;
+    ok = nd == 3 || nd == 4;
+    if (ok == 1) ok = whole_tensor(args[0], args[5], device, nd, q);
+    if (ok == 1 && nd == 3) { q[3] = q[2]; q[2] = 1; }
+    if (ok == 1) ok = q[0] == c[0] && q[3] == 64 * c[3];
+    if (ok != 1) return refused(ok, "q must be a contiguous bf16 tensor [B, Hq, n_q, d] or [B, Hq, d] matching the cache and on its GPU");
+    return Py_BuildValue("(lLLLLLL)", device, c[0], q[1], c[1], 64 * c[2], q[2], q[3]);
+}
+// check_norm_rope(q, k, v or None, bfloat16) -> (device, B, N, Hq, Hkv, d, strides of q, of k, of v)
+PyObject* check_norm_rope(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 4) return PyErr_Format(PyExc_TypeError, "expected 4 arguments, got %zd", n);
+    long device = -1;
+    long long q[4], k[4], v[4], qs[4], ks[4], vs[4] = {0, 0, 0, 0};
+    int ok = rows_tensor(args[0], args[3], device, q, qs);
+    if (ok == 1) ok = rows_tensor(args[1], args[3], device, k, ks);
+    if (ok == 1) ok = k[0] == q[0] && k[1] == q[1] && k[3] == q[3];
+    if (ok == 1 && args[2] != Py_None) {
+        ok = rows_tensor(args[2], args[3], device, v, vs);
+        if (ok == 1) ok = v[0] == k[0] && v[1] == k[1] && v[2] == k[2] && v[3] == k[3];
+    }
+    if (ok != 1) return refused(ok, "q [B, N, Hq, d], k and v [B, N, Hkv, d] must be bf16 tensors on one GPU, their last dimension contiguous");
+    return Py_BuildValue("(lLLLLLLLLLLLLLL)", device, q[0], q[1], q[2], k[2], q[3], qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2]);
+}
+// check_tensor(t, dtype, device, shape...): a contiguous tensor of that kind
+PyObject* check_tensor(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n < 4 || n > 9) return PyErr_Format(PyExc_TypeError, "expected 4 to 9 arguments, got %zd", n);
+    long device = PyLong_AsLong(args[2]);
+    if (device == -1 && PyErr_Occurred()) return nullptr;
+    long long want[6], have[6];
+    for (Py_ssize_t i = 3; i < n; ++i) {
+        want[i - 3] = PyLong_AsLongLong(args[i]);
+        if (want[i - 3] == -1 && PyErr_Occurred()) return nullptr;
+    }
+    int ok = whole_tensor(args[0], args[1], device, n - 3, have);
+    for (Py_ssize_t i = 0; ok == 1 && i < n - 3; ++i) ok = have[i] == want[i];
+    if (ok < 0) return nullptr;
+    return PyBool_FromLong(ok);
+}
+
 #define VFA_FUNCTION(f) (PyCFunction)(void (*)(void)) & f, METH_FASTCALL, nullptr
 #define VFA_METHOD(name) {#name, VFA_FUNCTION((Wrap<false, &name>::run))}
 #define VFA_METHODS(name) VFA_METHOD(name), {#name "_t", VFA_FUNCTION((Wrap<true, &name>::run))}
@@ -187,6 +314,8 @@ PyMethodDef methods[] = {
     VFA_METHODS(vfa_qk_norm_rope_fwd), VFA_METHODS(vfa_kv8_append), VFA_METHODS(vfa_kv8_read), VFA_METHOD(vfa_kv8_decode_splits),
     VFA_METHOD(vfa_kv8_decode_workspace_bytes), VFA_METHODS(vfa_kv8_decode_fwd),
     {"check_qkv", VFA_FUNCTION(check_qkv)}, {"check_cache", VFA_FUNCTION(check_cache)},
+    {"check_cache8", VFA_FUNCTION(check_cache8)}, {"check_kv8_append", VFA_FUNCTION(check_kv8_append)},
+    {"check_kv8_decode", VFA_FUNCTION(check_kv8_decode)}, {"check_norm_rope", VFA_FUNCTION(check_norm_rope)}, {"check_tensor", VFA_FUNCTION(check_tensor)},
     {"bytes_of", &bytes_of, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "The C ABI of libvfa.so.", -1, methods, nullptr, nullptr, nullptr, nullptr};

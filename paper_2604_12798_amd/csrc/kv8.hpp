@@ -30,6 +30,11 @@ __device__ __forceinline__ void kv8_values4(uint32_t w, float f, float* y) {
     const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
     y[0] = lo[0] * f; y[1] = lo[1] * f; y[2] = hi[0] * f; y[3] = hi[1] * f;
 }
+// codes 0 and 1 (HI: 2 and 3) of four -> bf16 values times a power of two
+template <typename HI>
+__device__ __forceinline__ uint32_t kv8_bf16x2(uint32_t w, float scale, HI) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, HI::value));
+}
 // smallest e >= kExpMin with a <= 448 * 2^e, a given by its bits (448 = 1.75 * 2^8)
 __device__ __forceinline__ int kv8_exponent(uint32_t bits) {
     const int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
@@ -57,11 +62,12 @@ __device__ __forceinline__ uint32_t wave_umax(uint32_t x) {
     return (uint32_t)__builtin_amdgcn_readfirstlane((int)max(b[0], b[1]));
 }
 
-// One workgroup per block that new rows may reach, KV head, keys or values.
+// A workgroup of 2 D threads per block that new rows may reach, KV head, keys or values.  Of keys a thread has two runs of 16 features (16 bytes of codes);
+// of values eight features of four neighbouring keys, whose codes are a dword of each feature's row, so that nothing has to be transposed: loads and
+// stores of 16 lanes cover 64 bytes of a row.  A thread is alone with its bytes of the cache; those it does not write it puts back.
 template <int D>
-__global__ __launch_bounds__(256) void kv8_append_kernel(const Kv8Append p) {
-    constexpr int CH = D / 8, NC = BN * CH / 256;  // runs of eight features of a row; of a thread
-    __shared__ uint32_t wmax[4];
+__global__ __launch_bounds__(2 * D) void kv8_append_kernel(const Kv8Append p) {
+    __shared__ uint32_t wmax[D / 32];
     const int side = blockIdx.y & 1, h = blockIdx.y >> 1, b = blockIdx.z;
     const int o = min(max(p.old_lens ? p.old_lens[b] : p.old_len, 0), p.n_cap);
     const int n = min(min(p.new_lens ? p.new_lens[b] : p.new_len, p.n_cap), o + p.n_in);
@@ -72,53 +78,99 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(const Kv8Append p) {
     uint8_t* const C = p.C[side] + blk * (BN * D);
     const uint16_t* const x = p.X[side] + b * p.sb[side] + h * p.sh[side] + (long long)(key0 - o) * p.sn[side];
     const int e_old = (int)p.S[side][blk] - 127;
-    u32x4 r[NC];
-    uint32_t a = 0;
+    // keys: run u of the thread is features kf to kf + 15 of key kk + 32 u; values: features vf to vf + 7 of keys vk to vk + 3
+    const int kk = threadIdx.x / (D / 16), kf = threadIdx.x % (D / 16) * 16, vk = threadIdx.x % 16 * 4, vf = threadIdx.x / 16 * 8;
+    // (no load sits behind a branch: rows that are not new read a new one again, dwords of values that stay the first that does not)
+    auto body = [&](auto side_c, auto whole_c) __attribute__((always_inline)) {
+        constexpr bool V = decltype(side_c)::value, WHOLE = decltype(whole_c)::value;  // WHOLE: every token of the block is new
+        uint32_t* const at4 = reinterpret_cast<uint32_t*>(C + vf * BN);
+        uint32_t w4[8];
+        u32x4 r[4];
 #pragma unroll
-    for (int i = 0; i < NC; ++i) {
-        const int c = i * 256 + threadIdx.x, key = c / CH, f = c % CH * 8;
-        r[i] = u32x4{0, 0, 0, 0};
-        if (key >= k0 && key < k1) r[i] = *reinterpret_cast<const u32x4*>(x + key * p.sn[side] + f);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint32_t lo = r[i][e] << 16 & 0x7fffffffu, hi = r[i][e] & 0x7fff0000u;
-            a = max(a, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
+        for (int i = 0; i < 4; ++i) {
+            const int key = V ? vk + i : kk + 32 * (i >> 1), f = V ? vf : kf + 8 * (i & 1);
+            r[i] = *reinterpret_cast<const u32x4*>(x + (WHOLE ? key : min(max(key, k0), k1 - 1)) * p.sn[V] + f);
         }
-    }
-    a = wave_umax(a);
-    if ((threadIdx.x & 63) == 0) wmax[threadIdx.x >> 6] = a;
-    __syncthreads();
-    int e = kv8_exponent(max(max(wmax[0], wmax[1]), max(wmax[2], wmax[3])));
-    const bool again = k0 > 0 && e > e_old;
-    if (k0 > 0) e = max(e, e_old);
-    const float f_new = ldexpf(1.f, -e), f_old = ldexpf(1.f, e_old - e);
+        if (V && !WHOLE) {
+            const int near = kv8_place(min(max(vk, k0), k1 - 1) & ~3) / 4;
 #pragma unroll
-    for (int i = 0; i < NC; ++i) {
-        const int c = i * 256 + threadIdx.x, key = c / CH, f = c % CH * 8;
-        const bool fresh = key >= k0 && key < k1;
-        if (!fresh && !(again && key < k0)) continue;
-        uint8_t* const at = side == 0 ? C + f / 64 * (64 * BN) + key * 64 + f % 64 : C + f * BN + kv8_place(key);
-        float y[8];
-        if (fresh) {
+            for (int q = 0; q < 8; ++q) w4[q] = at4[q * (BN / 4) + near];
+        }
+        uint32_t a = 0;  // (a new row that is read again does not change the largest)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                y[2 * q] = __uint_as_float(r[i][q] << 16) * f_new;
-                y[2 * q + 1] = __uint_as_float(r[i][q] & 0xffff0000u) * f_new;
+                const uint32_t lo = r[i][q] << 16 & 0x7fffffffu, hi = r[i][q] & 0x7fff0000u;
+                a = max(a, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
             }
-        } else {
-            u32x2 w = {0, 0};
-            if (side == 0) w = *reinterpret_cast<const u32x2*>(at);
-            else
-                for (int q = 0; q < 8; ++q) w[q / 4] |= (uint32_t)at[q * BN] << 8 * (q % 4);
-            kv8_values4(w[0], f_old, y);
-            kv8_values4(w[1], f_old, y + 4);
+        a = wave_umax(a);
+        if ((threadIdx.x & 63) == 0) wmax[threadIdx.x >> 6] = a;
+        __syncthreads();
+        a = wmax[0];
+#pragma unroll
+        for (int w = 1; w < D / 32; ++w) a = max(a, wmax[w]);
+        int e = kv8_exponent(a);
+        const bool again = !WHOLE && k0 > 0 && e > e_old;
+        if (!WHOLE && k0 > 0) e = max(e, e_old);
+        const float f_new = ldexpf(1.f, -e), f_old = ldexpf(1.f, e_old - e);
+        const int first = again ? 0 : k0;  // keys [first, k1) are written
+        if (!V) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int key = kk + 32 * u;
+                if (!WHOLE && (key < first || key >= k1)) continue;
+                u32x4* const at = reinterpret_cast<u32x4*>(C + kf / 64 * (64 * BN) + key * 64 + kf % 64);
+                float y[16];
+                if (WHOLE || key >= k0) {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        const uint32_t w = r[2 * u + (q >> 2)][q & 3];
+                        y[2 * q] = __uint_as_float(w << 16) * f_new;
+                        y[2 * q + 1] = __uint_as_float(w & 0xffff0000u) * f_new;
+                    }
+                } else {
+                    const u32x4 w = *at;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) kv8_values4(w[q], f_old, y + 4 * q);
+                }
+                *at = u32x4{kv8_codes4(y), kv8_codes4(y + 4), kv8_codes4(y + 8), kv8_codes4(y + 12)};
+            }
+        } else if (WHOLE || (vk < k1 && vk + 4 > first)) {
+            uint32_t put = 0;  // bytes that are written
+            if (!WHOLE) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (vk + i >= first && vk + i < k1) put |= 0xffu << 8 * i;
+                if (vk + 4 <= k0)  // (old ones alone, coded again)
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) w4[q] = at4[q * (BN / 4) + kv8_place(vk) / 4];
+            }
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                float y[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[i] = __uint_as_float(q & 1 ? r[i][q >> 1] & 0xffff0000u : r[i][q >> 1] << 16) * f_new;
+                if (!WHOLE) {
+                    float v[4];
+                    kv8_values4(w4[q], f_old, v);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) y[i] = vk + i < k0 ? v[i] : y[i];
+                }
+                const uint32_t w = kv8_codes4(y);
+                w4[q] = WHOLE ? w : (w4[q] & ~put) | (w & put);
+            }
+#pragma unroll
+            for (int q = 0; q < 8; ++q) at4[q * (BN / 4) + kv8_place(vk) / 4] = w4[q];
         }
-        const u32x2 w = {kv8_codes4(y), kv8_codes4(y + 4)};
-        if (side == 0) *reinterpret_cast<u32x2*>(at) = w;
-        else
-            for (int q = 0; q < 8; ++q) at[q * BN] = (uint8_t)(w[q / 4] >> 8 * (q % 4));
-    }
-    if (threadIdx.x == 0) p.S[side][blk] = (uint8_t)(e + 127);
+        if (threadIdx.x == 0) p.S[V][blk] = (uint8_t)(e + 127);
+    };
+    using std::true_type, std::false_type;
+    const bool whole = k0 == 0 && k1 == BN;
+    if (side == 0 && whole) body(false_type{}, true_type{});
+    else if (side == 0) body(false_type{}, false_type{});
+    else if (whole) body(true_type{}, true_type{});
+    else body(true_type{}, false_type{});
 }
 
 struct Kv8Read {
@@ -129,33 +181,63 @@ struct Kv8Read {
     int seq_len, n, n_cap, T, Hkv;
 };
 
-// One workgroup per block, KV head, keys or values; rows past the sequence's end are zeros.
+// A workgroup per block, KV head, keys or values, with the threads' shares as in kv8_append_kernel; rows past the sequence's end are zeros.
 template <int D>
-__global__ __launch_bounds__(256) void kv8_read_kernel(const Kv8Read p) {
-    constexpr int CH = D / 8, NC = BN * CH / 256;
+__global__ __launch_bounds__(2 * D) void kv8_read_kernel(const Kv8Read p) {
     const int side = blockIdx.y & 1, h = blockIdx.y >> 1, b = blockIdx.z;
     const int len = min(max(p.seq_lens ? p.seq_lens[b] : p.seq_len, 0), p.n_cap), key0 = blockIdx.x * BN;
+    const int live = min(len - key0, BN), rows = min(p.n - key0, BN);  // keys that there are; rows to write
     const size_t blk = ((size_t)b * p.Hkv + h) * p.T + blockIdx.x;
     const uint8_t* const C = p.C[side] + blk * (BN * D);
-    const float f = key0 < len ? ldexpf(1.f, (int)p.S[side][blk] - 127) : 0.f;
+    const float f = live > 0 ? ldexpf(1.f, (int)p.S[side][blk] - 127) : 0.f;
+    uint16_t* const y = p.Y[side] + (((size_t)b * p.Hkv + h) * p.n + key0) * D;
+    if (side == 0) {
+        const int kk = threadIdx.x / (D / 16), kf = threadIdx.x % (D / 16) * 16;
+        u32x4 w[2];
 #pragma unroll
-    for (int i = 0; i < NC; ++i) {
-        const int c = i * 256 + threadIdx.x, key = c / CH, ft = c % CH * 8;
-        if (key0 + key >= p.n) continue;
-        u32x4 r = {0, 0, 0, 0};
-        if (key0 + key < len) {
-            const uint8_t* const at = side == 0 ? C + ft / 64 * (64 * BN) + key * 64 + ft % 64 : C + ft * BN + kv8_place(key);
-            u32x2 w = {0, 0};
-            if (side == 0) w = *reinterpret_cast<const u32x2*>(at);
-            else
-                for (int q = 0; q < 8; ++q) w[q / 4] |= (uint32_t)at[q * BN] << 8 * (q % 4);
-            float y[8];
-            kv8_values4(w[0], f, y);
-            kv8_values4(w[1], f, y + 4);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) r[q] = pack_bf16(y[2 * q], y[2 * q + 1]);
+        for (int u = 0; u < 2; ++u) {
+            w[u] = u32x4{0, 0, 0, 0};
+            if (kk + 32 * u < live) w[u] = *reinterpret_cast<const u32x4*>(C + kf / 64 * (64 * BN) + (kk + 32 * u) * 64 + kf % 64);
         }
-        *reinterpret_cast<u32x4*>(p.Y[side] + (((size_t)b * p.Hkv + h) * p.n + key0 + key) * D + ft) = r;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            if (kk + 32 * u >= rows) continue;
+            u32x4 v[2];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                v[q >> 1][2 * (q & 1)] = kv8_bf16x2(w[u][q], f, std::false_type{});
+                v[q >> 1][2 * (q & 1) + 1] = kv8_bf16x2(w[u][q], f, std::true_type{});
+            }
+            u32x4* const at = reinterpret_cast<u32x4*>(y + (size_t)(kk + 32 * u) * D + kf);
+            at[0] = v[0];
+            at[1] = v[1];
+        }
+    } else {
+        const int vk = threadIdx.x % 16 * 4, vf = threadIdx.x / 16 * 8;
+        uint32_t w[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) w[q] = 0;
+        if (vk < live) {
+            const uint32_t* const at = reinterpret_cast<const uint32_t*>(C + vf * BN + kv8_place(vk));
+#pragma unroll
+            for (int q = 0; q < 8; ++q) w[q] = at[q * (BN / 4)];
+        }
+        uint32_t v[2][8];  // features of keys 0 and 1, 2 and 3
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            v[0][q] = kv8_bf16x2(w[q], f, std::false_type{});
+            v[1][q] = kv8_bf16x2(w[q], f, std::true_type{});
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (vk + i >= rows) continue;
+            u32x4 o = {0, 0, 0, 0};
+            if (vk + i < live)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    o[q] = __builtin_amdgcn_perm(v[i >> 1][2 * q + 1], v[i >> 1][2 * q], i & 1 ? 0x07060302u : 0x05040100u);
+            *reinterpret_cast<u32x4*>(y + (size_t)(vk + i) * D + vf) = o;
+        }
     }
 }
 

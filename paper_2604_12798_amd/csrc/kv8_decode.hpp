@@ -29,9 +29,9 @@ struct Kv8Decode {
 
 // eight codes -> bf16 values
 __device__ __forceinline__ bf16x8 kv8_bf16x8(uint32_t w0, uint32_t w1, float scale) {
-    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, true);
-    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, true);
-    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+    using std::true_type, std::false_type;
+    return __builtin_bit_cast(bf16x8, u32x4{kv8_bf16x2(w0, scale, false_type{}), kv8_bf16x2(w0, scale, true_type{}),
+                                            kv8_bf16x2(w1, scale, false_type{}), kv8_bf16x2(w1, scale, true_type{})});
 }
 __device__ __forceinline__ float kg_max(float x) {  // over the four lanes of a row
     const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);

@@ -20,7 +20,6 @@ struct RopeParams {
     const int* first_pos;    // [B] or null
     int first, n_pos, rot, N, tokens;  // tokens = B * N
     int Hq, Hkv, heads;      // heads = Hq + Hkv (+ Hkv with values)
-    int per;                 // heads that a workgroup does one after the other
     float eps;
 };
 
@@ -46,7 +45,21 @@ __device__ __forceinline__ float row_sum(float x) {
     return x;
 }
 
-template <int D, bool NORM, int PAIRS>
+template <bool STREAM>
+__device__ __forceinline__ u32x4 rope_load(const uint16_t* x) {
+    const u32x4* const at = reinterpret_cast<const u32x4*>(x);
+    return STREAM ? __builtin_nontemporal_load(at) : *at;
+}
+template <bool STREAM>
+__device__ __forceinline__ void rope_store(uint16_t* y, const u32x4& v) {
+    u32x4* const at = reinterpret_cast<u32x4*>(y);
+    if (STREAM) __builtin_nontemporal_store(v, at);
+    else *at = v;
+}
+
+// PER heads of a thread, one after the other, their loads first; STREAM: more data than the memory-side cache holds, which the kernel behind this
+// one will not find there anyway, goes past it
+template <int D, bool NORM, int PAIRS, int PER, bool STREAM>
 __global__ __launch_bounds__(256) void norm_rope_kernel(const RopeParams p) {
     constexpr int L = D / 16, ROWS = 256 / L;  // lanes of a row; tokens of a workgroup
     const int j = threadIdx.x % L;
@@ -61,23 +74,37 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(const RopeParams p) {
     if (PAIRS != PAIRS_NONE) {
         const int pos = (int)min(max((long long)n + (p.first_pos ? p.first_pos[b] : p.first), 0LL), (long long)p.n_pos - 1);
         const float* const c = p.cos_sin + (size_t)pos * p.rot;
+        const int at = j < pairs8 ? 8 * j : 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            cs[e] = j < pairs8 ? c[8 * j + e] : 1.f;
-            sn[e] = j < pairs8 ? c[p.rot / 2 + 8 * j + e] : 0.f;
+        for (int e4 = 0; e4 < 2; ++e4) {
+            const f32x4 x = *reinterpret_cast<const f32x4*>(c + at + 4 * e4), y = *reinterpret_cast<const f32x4*>(c + p.rot / 2 + at + 4 * e4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                cs[4 * e4 + e] = j < pairs8 ? x[e] : 1.f;
+                sn[4 * e4 + e] = j < pairs8 ? y[e] : 0.f;
+            }
         }
     }
-    const int h1 = min(p.heads, ((int)blockIdx.y + 1) * p.per);
-    for (int hh = blockIdx.y * p.per; hh < h1; ++hh) {
-        const int kind = hh < p.Hq ? 0 : hh < p.Hq + p.Hkv ? 1 : 2;  // (the same in all lanes)
-        const int h = kind == 0 ? hh : kind == 1 ? hh - p.Hq : hh - p.Hq - p.Hkv, H = kind == 0 ? p.Hq : p.Hkv;
-        const uint16_t* const x = p.X[kind] + b * p.sb[kind] + n * p.sn[kind] + h * p.sh[kind];
-        uint16_t* const y = p.Y[kind] + (((size_t)b * H + h) * p.N + n) * D;
-        u32x4 ra = *reinterpret_cast<const u32x4*>(x + 8 * ca), rb = *reinterpret_cast<const u32x4*>(x + 8 * cb);
+    const int h0 = blockIdx.y * PER;
+    u32x4 ra[PER], rb[PER];
+    auto side = [&](int hh) { return hh < p.Hq ? 0 : hh < p.Hq + p.Hkv ? 1 : 2; };  // (the same in all lanes)
+    auto head = [&](int hh, int kind) { return kind == 0 ? hh : kind == 1 ? hh - p.Hq : hh - p.Hq - p.Hkv; };
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+        const int hh = min(h0 + u, p.heads - 1), kind = side(hh);
+        const uint16_t* const x = p.X[kind] + b * p.sb[kind] + n * p.sn[kind] + head(hh, kind) * p.sh[kind];
+        ra[u] = rope_load<STREAM>(x + 8 * ca);
+        rb[u] = rope_load<STREAM>(x + 8 * cb);
+    }
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+        const int hh = h0 + u, kind = side(hh);
+        if (hh >= p.heads) break;
+        uint16_t* const y = p.Y[kind] + (((size_t)b * (kind == 0 ? p.Hq : p.Hkv) + head(hh, kind)) * p.N + n) * D;
         if (kind < 2) {
             float a[8], c[8];
-            unpack_bf16(ra, a);
-            unpack_bf16(rb, c);
+            unpack_bf16(ra[u], a);
+            unpack_bf16(rb[u], c);
             if (NORM) {
                 float ss = 0.f;
 #pragma unroll
@@ -113,12 +140,12 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(const RopeParams p) {
                     c[2 * e + 1] = z1 * cs[4 + e] + z0 * sn[4 + e];
                 }
             }
-            ra = pack_bf16x8(a);
-            rb = pack_bf16x8(c);
+            ra[u] = pack_bf16x8(a);
+            rb[u] = pack_bf16x8(c);
         }
         if (live) {
-            *reinterpret_cast<u32x4*>(y + 8 * ca) = ra;
-            *reinterpret_cast<u32x4*>(y + 8 * cb) = rb;
+            rope_store<STREAM>(y + 8 * ca, ra[u]);
+            rope_store<STREAM>(y + 8 * cb, rb[u]);
         }
     }
 }

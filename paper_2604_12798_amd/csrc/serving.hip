@@ -69,22 +69,33 @@ int vfa_qk_norm_rope_fwd(const void* Xq, const void* Xk, const void* Xv, void* Q
     p.N = N; p.tokens = (int)tokens; p.Hq = Hq; p.Hkv = Hkv; p.heads = (int)heads; p.eps = eps;
     const int rows = 256 / (d / 16);
     const long long wgs = (tokens + rows - 1) / rows;
-    p.per = 4;
-    const long long ys = (heads + p.per - 1) / p.per;
+    // Heads of a thread: four, or one where that gives fewer than two workgroups for each compute unit (16 x 1 tokens of 48 heads: 6.3 / 4.2 us).
+    // Loads and stores past the caches from 256 MiB on (2 x 16384 tokens of 48 heads, 768 MiB, 178 / 164 us; 3 x 777 of 24, d = 64, 14 MiB,
+    // 5.7 / 6.2)
+    const int n_cu = cu_count() > 0 ? cu_count() : 256;
+    const bool few = wgs * ((heads + 3) / 4) < 2 * n_cu, stream_past = tokens * heads * d >= 1LL << 26;
+    const long long ys = few ? heads : (heads + 3) / 4;
     if (ys > 65535 || wgs * ys > kMaxWorkgroups256) return VFA_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)wgs, (unsigned)ys);
     hipStream_t s = (hipStream_t)stream;
     (void)hipGetLastError();
     with_d(d, [&](auto d_c) {
         constexpr int D = decltype(d_c)::value;
-        auto launch = [&](auto norm_c) {
-            constexpr bool NORM = decltype(norm_c)::value;
-            if (rot_dim == 0) norm_rope_kernel<D, NORM, PAIRS_NONE><<<grid, 256, 0, s>>>(p);
-            else if (interleaved) norm_rope_kernel<D, NORM, PAIRS_NEXT><<<grid, 256, 0, s>>>(p);
-            else norm_rope_kernel<D, NORM, PAIRS_HALF><<<grid, 256, 0, s>>>(p);
+        auto launch = [&](auto norm_c, auto per_c, auto past_c) {
+            constexpr bool NORM = decltype(norm_c)::value, PAST = decltype(past_c)::value;
+            constexpr int PER = decltype(per_c)::value;
+            if (rot_dim == 0) norm_rope_kernel<D, NORM, PAIRS_NONE, PER, PAST><<<grid, 256, 0, s>>>(p);
+            else if (interleaved) norm_rope_kernel<D, NORM, PAIRS_NEXT, PER, PAST><<<grid, 256, 0, s>>>(p);
+            else norm_rope_kernel<D, NORM, PAIRS_HALF, PER, PAST><<<grid, 256, 0, s>>>(p);
         };
-        if (norm) launch(std::true_type{});
-        else launch(std::false_type{});
+        auto sized = [&](auto norm_c) {
+            using std::integral_constant;
+            if (few) launch(norm_c, integral_constant<int, 1>{}, std::false_type{});
+            else if (stream_past) launch(norm_c, integral_constant<int, 4>{}, std::true_type{});
+            else launch(norm_c, integral_constant<int, 4>{}, std::false_type{});
+        };
+        if (norm) sized(std::true_type{});
+        else sized(std::false_type{});
     });
     return launched();
 }
@@ -112,7 +123,7 @@ int vfa_kv8_append(const void* K, const void* V, void* K8, void* V8, void* KS, v
     if (tiles * 2 * Hkv * B > kMaxWorkgroups256) return VFA_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)tiles, (unsigned)(2 * Hkv), (unsigned)B);
     (void)hipGetLastError();
-    with_d(d, [&](auto d_c) { kv8_append_kernel<decltype(d_c)::value><<<grid, 256, 0, (hipStream_t)stream>>>(p); });
+    with_d(d, [&](auto d_c) { kv8_append_kernel<decltype(d_c)::value><<<grid, 2 * d, 0, (hipStream_t)stream>>>(p); });
     return launched();
 }
 
@@ -131,7 +142,7 @@ int vfa_kv8_read(const void* K8, const void* V8, const void* KS, const void* VS,
     if (tiles * 2 * Hkv * B > kMaxWorkgroups256) return VFA_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)tiles, (unsigned)(2 * Hkv), (unsigned)B);
     (void)hipGetLastError();
-    with_d(d, [&](auto d_c) { kv8_read_kernel<decltype(d_c)::value><<<grid, 256, 0, (hipStream_t)stream>>>(p); });
+    with_d(d, [&](auto d_c) { kv8_read_kernel<decltype(d_c)::value><<<grid, 2 * d, 0, (hipStream_t)stream>>>(p); });
     return launched();
 }
 
