@@ -381,8 +381,9 @@ int vfa_kv8_append(const void* K, const void* V, void* K8, void* V8, void* KS, v
 int vfa_kv8_read(const void* K8, const void* V8, const void* KS, const void* VS, void* K, void* V, int B, int Hkv,
                  int n_cap, int n, int d, const int* seq_lens, int seq_len, void* stream);
 
-/* A number of key ranges for vfa_kv8_decode_fwd that suits a batch of sequences of up to n_keys tokens. */
-int vfa_kv8_decode_splits(int B, int Hkv, int n_keys);
+/* A number of key ranges for vfa_kv8_decode_fwd that suits a batch of sequences of n_keys tokens each (varlen = 0), or of lengths of their
+ * own up to n_keys (varlen = 1), on the current device. */
+int vfa_kv8_decode_splits(int B, int Hq, int Hkv, int n_q, int d, int n_keys, int varlen);
 
 /* Bytes of workspace vfa_kv8_decode_fwd needs for n_splits > 1. */
 size_t vfa_kv8_decode_workspace_bytes(int B, int Hq, int n_q, int d, int n_splits);

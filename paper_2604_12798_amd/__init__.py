@@ -99,7 +99,7 @@ def lib() -> ctypes.CDLL:
         L.vfa_kv8_read.restype = i
         L.vfa_kv8_read.argtypes = [vp] * 6 + [i] * 5 + [vp, i, vp]
         L.vfa_kv8_decode_splits.restype = i
-        L.vfa_kv8_decode_splits.argtypes = [i, i, i]
+        L.vfa_kv8_decode_splits.argtypes = [i] * 7
         L.vfa_kv8_decode_workspace_bytes.restype = sz
         L.vfa_kv8_decode_workspace_bytes.argtypes = [i, i, i, i, i]
         L.vfa_kv8_decode_fwd.restype = i
@@ -454,7 +454,7 @@ def mxfp4_attn_fwd(Q4, QS, K4, KS, Vt8, *, descale_v, frozen=True, block_m=128, 
     return O, L, ws
 
 
-_empty = _f32 = _u8 = _tensor = None
+_empty_like = _f32 = _u8 = _tensor = None
 
 
 def _serving(device):
@@ -465,10 +465,10 @@ def _serving(device):
 
 def _ns():
     """_n(), and what the wrappers of the serving operators use of torch on every call."""
-    global _empty, _f32, _u8, _tensor, _current_device, _current_stream
-    if _empty is None:
+    global _empty_like, _f32, _u8, _tensor, _current_device, _current_stream
+    if _empty_like is None:
         import torch
-        _empty, _f32, _u8, _tensor = torch.empty, torch.float32, torch.uint8, torch.Tensor
+        _empty_like, _f32, _u8, _tensor = torch.empty_like, torch.float32, torch.uint8, torch.Tensor
         _current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
     return _native or _n()
 
@@ -506,7 +506,7 @@ def qk_norm_rope_fwd(q, k, v=None, *, norm=True, q_weight=None, k_weight=None, e
     at, first = _lengths(first_pos, n, B, dev, "first_pos")
     if out is None:
         Q, K = q.new_empty((B, Hq, N, d)), q.new_empty((B, Hkv, N, d))
-        V = None if v is None else q.new_empty((B, Hkv, N, d))
+        V = None if v is None else _empty_like(K)
     else:
         Q, K, V = out
         _need(n.check_tensor(Q, _bf16, dev, B, Hq, N, d) and n.check_tensor(K, _bf16, dev, B, Hkv, N, d)
@@ -555,7 +555,8 @@ def kv8_read(cache, n: int, *, seq_lens=None, out=None, stream=None):
     _need(0 <= n <= n_cap, f"n must be between 0 and the cache's {n_cap} tokens")
     lens, length = _lengths(n if seq_lens is None else seq_lens, nat, B, dev, "seq_lens")
     if out is None:
-        K, V = K8.new_empty((B, Hkv, n, d), dtype=_bf16), K8.new_empty((B, Hkv, n, d), dtype=_bf16)
+        K = K8.new_empty((B, Hkv, n, d), dtype=_bf16)
+        V = _empty_like(K)
     else:
         K, V = out
         _need(nat.check_tensor(K, _bf16, dev, B, Hkv, n, d) and nat.check_tensor(V, _bf16, dev, B, Hkv, n, d),
@@ -570,8 +571,9 @@ def kv8_decode_workspace_bytes(B: int, Hq: int, n_q: int, d: int, n_splits: int)
     return int(_n().vfa_kv8_decode_workspace_bytes(B, Hq, n_q, d, n_splits))
 
 
-def kv8_decode_splits(B: int, Hkv: int, n_keys: int) -> int:
-    return int(_n().vfa_kv8_decode_splits(B, Hkv, n_keys))
+def kv8_decode_splits(B: int, Hq: int, Hkv: int, n_q: int, d: int, n_keys: int, varlen: bool = False) -> int:
+    """Key ranges that suit a batch of n_keys tokens each, or (varlen) of lengths of their own up to n_keys."""
+    return int(_n().vfa_kv8_decode_splits(B, Hq, Hkv, n_q, d, n_keys, int(bool(varlen))))
 
 
 def kv8_decode_fwd(q, cache, seq_lens, *, n_splits=None, softmax_scale=0.0, workspace=None, out=None, lse=None, want_lse=True, stream=None):
@@ -583,9 +585,11 @@ def kv8_decode_fwd(q, cache, seq_lens, *, n_splits=None, softmax_scale=0.0, work
     dev, B, Hq, Hkv, n_cap, n_q, d = n.check_kv8_decode(q, K8, V8, KS, VS, _bf16, _u8)
     _serving(dev)
     lens, n_keys = _lengths(seq_lens, n, B, dev, "seq_lens")
-    n_splits = n.vfa_kv8_decode_splits(B, Hkv, n_cap if lens is not None else n_keys) if n_splits is None else int(n_splits)
+    if n_splits is None:
+        n_splits = n.vfa_kv8_decode_splits(B, Hq, Hkv, n_q, d, n_keys if lens is None else n_cap, int(lens is not None))
+    n_splits = int(n_splits)
     if out is None:
-        out = q.new_empty(q.shape)
+        out = _empty_like(q)
     else:
         _need(n.check_tensor(out, _bf16, dev, *q.shape), "out must be a contiguous bf16 tensor of q's shape on the same GPU")
     if lse is not None:

@@ -176,18 +176,16 @@ PyObject* bytes_of(PyObject*, PyObject* t) {
 
 // The serving operators' tensors: 1, 0, or -1 with an error set, as above.  All of them lie on one GPU, whose index goes to `device` (-1 at first).
 int on_device(PyObject* t, PyObject* dtype, long& device) {
-    int ok = truth(attribute(t, names.is_cuda));
-    if (ok != 1) return ok;
     {
         const Ref d = attribute(t, names.dtype);
-        ok = d.o ? PyObject_RichCompareBool(d.o, dtype, Py_EQ) : -1;
+        const int ok = d.o ? PyObject_RichCompareBool(d.o, dtype, Py_EQ) : -1;
         if (ok != 1) return ok;
     }
     const Ref i = method(t, names.get_device);
     const long at = i.o ? PyLong_AsLong(i.o) : -1;
     if (at == -1 && PyErr_Occurred()) return -1;
     if (device < 0) device = at;
-    return at == device;
+    return at >= 0 && at == device;  // (-1: a tensor of the host)
 }
 // ... of `n` dimensions, contiguous; the shape goes to v
 int whole_tensor(PyObject* t, PyObject* dtype, long& device, Py_ssize_t n, long long* v) {

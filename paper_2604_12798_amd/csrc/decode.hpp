@@ -35,7 +35,10 @@ struct DecodeParams {
     int g, per;  // query heads per KV head; tiles of a range where the batch has one length
     const int* seq_lens;    // null, or [B] device array: valid keys per batch entry (clamped to [1, n_cap]) instead of n_keys
     float c;
+    int* dealt;  // SLOTS_TABLE: [B, 2] the ranges of the entries before b, its own number of ranges
 };
+// Where the merge finds the ranges of an entry: n_splits each; by the search of the split kernel; in a table that the split kernel wrote.
+enum Slots { SLOTS_FIXED = 0, SLOTS_SEARCH = 1, SLOTS_TABLE = 2 };
 
 // What the entries of a batch have: one length; lengths of their own and n_splits ranges each; lengths of their own and ranges
 // dealt out by length.
@@ -290,17 +293,20 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 2 : 1) void decode_split_kernel(c
 // 5.0, now 2.7 and 4.8.  Only the rounds that the ranges fill: steps of 6400 heads of two ranges of 100 keys, four rounds of loads for
 // each / one, d = 64 16.8 / 14.4, d = 128 29.2 / 26.8.)
 // (NANS: a row whose sum is NaN has that for its LSE, not -inf)
-template <int D, bool DEALT, bool NANS = false>
+template <int D, int SLOTS, bool NANS = false>
 __global__ __launch_bounds__(256) void decode_merge_kernel(const DecodeParams p) {
     constexpr int C4 = D / 4, NG = 256 / C4;
     __shared__ float xo[NG][D], xm[NG], xl[NG];
     const int h = blockIdx.x, b = blockIdx.y, row = b * p.Hq + h;
     const int c4 = threadIdx.x % C4, gr = threadIdx.x / C4;
     int first = b * p.n_splits, nb = p.n_splits;
-    if (DEALT) {
+    if (SLOTS == SLOTS_SEARCH) {
         const Ranges rg = varlen_find(p, threadIdx.x & 63, -1, b);
         first = rg.first;
         nb = rg.nb;
+    } else if (SLOTS == SLOTS_TABLE) {
+        first = p.dealt[2 * b];
+        nb = p.dealt[2 * b + 1];
     }
     const float* const pm0 = p.pm + (size_t)first * p.Hq + h;
     const float* const pl0 = p.lpart + (size_t)first * p.Hq + h;

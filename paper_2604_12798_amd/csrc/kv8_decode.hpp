@@ -15,8 +15,8 @@ namespace {
 // passes through LDS; only the waves' results meet there.  A wave requests a tile's keys when those of the one before are converted and its
 // values likewise, so that 8 to 16 KiB (D = 128) are on their way to each wave all the time.
 // Token t of the n_q sees keys < len - n_q + 1 + t.  What lies behind a sequence's end is neither a key (its scores are -inf) nor a value (its
-// codes are cleared: 0 * NaN).  A NaN in the value of a key that only some of the tokens see would reach the others through weights of zero:
-// where there is one, each token has its own product (with the keys that it does not see cleared).
+// codes are cleared: 0 * NaN).  A NaN in the value of a key that only some of the tokens see would reach the others through weights of zero: it is
+// cleared, too, and the sums of those who see it are set.
 // Partial sums of ranges and their merge: decode.hpp, a row for a head.
 struct Kv8Decode {
     DecodeParams d;  // Hq, g: rows for heads (query heads times new tokens); K, V not used
@@ -64,6 +64,10 @@ __global__ __launch_bounds__(64 * W, RT == 1 ? 3 : 2) void kv8_decode_kernel(con
         const Ranges rg = varlen_find(p, lane, w, 0);
         if (rg.b < 0) return;  // (the same in all waves of the workgroup)
         b = rg.b; r = w - rg.first; nb = rg.nb;
+        if (r == 0 && hkv == 0 && threadIdx.x == 0) {  // (every entry has a range)
+            p.dealt[2 * b] = rg.first;
+            p.dealt[2 * b + 1] = nb;
+        }
     }
     const size_t slot = (size_t)w * p.Hq + hkv * rows;
     const int len = LENS == LENS_ONE ? p.n_keys : __builtin_amdgcn_readfirstlane(min(max(p.seq_lens[b], 0), p.n_cap));
@@ -106,7 +110,8 @@ __global__ __launch_bounds__(64 * W, RT == 1 ? 3 : 2) void kv8_decode_kernel(con
         sv = VS[min(t, r1 - 1)];
         kv8_request<NI>(V8 + (size_t)t * BYTES, want(t), off, rv);
     };
-    // tile t; EDGE: some row does not see all of it
+    // tile t; EDGE: some row does not see all of it (there are two such tiles at most, so a wave has one at most, as its last)
+    static_assert(W >= 2, "the two tiles that some rows see in part are the last of two waves");
     auto body = [&](int t, auto edge_c) __attribute__((always_inline)) {
         constexpr bool EDGE = decltype(edge_c)::value;
         f32x4 st[RT][4];
@@ -127,19 +132,20 @@ __global__ __launch_bounds__(64 * W, RT == 1 ? 3 : 2) void kv8_decode_kernel(con
             }
         }
         __builtin_amdgcn_sched_barrier(0);  // (requests go out where they are written)
-        request_k(t + W);
+        if (!EDGE) request_k(t + W);
         __builtin_amdgcn_sched_barrier(0);
         const int key0 = t * BN;
-        bf16x8 pf[RT][2];
+        if (EDGE) {
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            if (EDGE) {
+            for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
                 for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (key0 + 16 * kt + 4 * kg + e >= sees[rt]) st[rt][kt][e] = -INFINITY;
-            }
+                    for (int e = 0; e < 4; ++e) st[rt][kt][e] = key0 + 16 * kt + 4 * kg + e < sees[rt] ? st[rt][kt][e] : -INFINITY;
+        }
+        bf16x8 pf[RT][2];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
             float mx = -INFINITY;
 #pragma unroll
             for (int kt = 0; kt < 4; ++kt)
@@ -175,57 +181,67 @@ __global__ __launch_bounds__(64 * W, RT == 1 ? 3 : 2) void kv8_decode_kernel(con
             const int left = end - (key0 + 16 * kt + 4 * kg);
             return left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << 8 * left) - 1;
         };
-        bool apart = false;  // tokens have a product each
+        auto nans = [](uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; };  // the top bits of the bytes that are NaN
         if (EDGE) {
-            uint32_t nan = 0;
+            uint32_t in[4], some[4], nan = 0;  // bytes of keys before the end; of keys that some rows see and others not
 #pragma unroll
             for (int kt = 0; kt < 4; ++kt) {
-                const uint32_t in = seen_bytes(kt, len), some = in & ~seen_bytes(kt, all_see);
+                in[kt] = seen_bytes(kt, len);
+                some[kt] = in[kt] & ~seen_bytes(kt, all_see);
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) {
-                    rv[dt][kt] &= in;
-                    nan |= ((rv[dt][kt] & some & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+                    rv[dt][kt] &= in[kt];
+                    nan |= nans(rv[dt][kt]) & some[kt];
                 }
             }
-            apart = __builtin_amdgcn_ballot_w64(nan != 0) != 0;
-        }
-        if (!apart) {
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
-                const bf16x8 v0 = kv8_bf16x8(rv[dt][0], rv[dt][1], vs), v1 = kv8_bf16x8(rv[dt][2], rv[dt][3], vs);
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    ot[rt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pf[rt][0], ot[rt][dt], 0, 0, 0);
-                    ot[rt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pf[rt][1], ot[rt][dt], 0, 0, 0);
-                }
-            }
-        } else {
-            for (int tok = 0; tok < P.n_q; ++tok) {
-                const int end = all_see + tok;
-                const uint32_t c0 = seen_bytes(0, end), c1 = seen_bytes(1, end), c2 = seen_bytes(2, end), c3 = seen_bytes(3, end);
+            if (__builtin_expect(__builtin_amdgcn_ballot_w64(nan != 0) != 0, 0)) {
+                // the NaNs of those keys leave the tile; their sums are set to NaN in the rows that see one, which a product of ones counts
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) {
-                    const bf16x8 v0 = kv8_bf16x8(rv[dt][0] & c0, rv[dt][1] & c1, vs), v1 = kv8_bf16x8(rv[dt][2] & c2, rv[dt][3] & c3, vs);
+                    uint32_t one[4];
+#pragma unroll
+                    for (int kt = 0; kt < 4; ++kt) {
+                        const uint32_t n = (nans(rv[dt][kt]) & some[kt]) >> 7;
+                        one[kt] = n * 0x38;  // (the code of 1)
+                        rv[dt][kt] &= ~(n * 0xff);
+                    }
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt) {
-                        f32x4 o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pf[rt][0], ot[rt][dt], 0, 0, 0);
-                        o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pf[rt][1], o, 0, 0, 0);
-                        if (sees[rt] == end) ot[rt][dt] = o;
+                        uint32_t see[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int k = key0 + 16 * (i >> 1) + 4 * kg + 2 * (i & 1);
+                            see[i] = (k < sees[rt] ? 0x3f80u : 0u) | (k + 1 < sees[rt] ? 0x3f800000u : 0u);
+                        }
+                        f32x4 count = {0.f, 0.f, 0.f, 0.f};
+                        count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kv8_bf16x8(one[0], one[1], 1.f), __builtin_bit_cast(bf16x8, u32x4{see[0], see[1], see[2], see[3]}), count, 0, 0, 0);
+                        count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kv8_bf16x8(one[2], one[3], 1.f), __builtin_bit_cast(bf16x8, u32x4{see[4], see[5], see[6], see[7]}), count, 0, 0, 0);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) ot[rt][dt][e] = count[e] > 0.f ? __builtin_nanf("") : ot[rt][dt][e];
                     }
                 }
             }
         }
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+            const bf16x8 v0 = kv8_bf16x8(rv[dt][0], rv[dt][1], vs), v1 = kv8_bf16x8(rv[dt][2], rv[dt][3], vs);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                ot[rt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pf[rt][0], ot[rt][dt], 0, 0, 0);
+                ot[rt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pf[rt][1], ot[rt][dt], 0, 0, 0);
+            }
+        }
         __builtin_amdgcn_sched_barrier(0);
-        request_v(t + W);
+        if (!EDGE) request_v(t + W);
         __builtin_amdgcn_sched_barrier(0);
     };
     int t = r0 + wave;
     if (t < r1) {
         request_k(t);
         request_v(t);
-        const int whole = all_see < 0 ? 0 : all_see / BN;  // tiles below are seen whole by every row
-        for (; t < min(r1, whole); t += W) body(t, std::false_type{});
-        for (; t < r1; t += W) body(t, std::true_type{});
+        const int whole = min(r1, all_see < 0 ? 0 : all_see / BN);  // tiles below are seen whole by every row
+        for (; t < whole; t += W) body(t, std::false_type{});
+        if (t < r1) body(t, std::true_type{});
     }
     // the waves' sums meet in LDS
     float* const ox = ex + wave * WS;

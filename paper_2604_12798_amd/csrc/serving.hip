@@ -146,16 +146,25 @@ int vfa_kv8_read(const void* K8, const void* V8, const void* KS, const void* VS,
     return launched();
 }
 
-int vfa_kv8_decode_splits(int B, int Hkv, int n_keys) {
-    if (B <= 0 || Hkv <= 0 || n_keys <= 0) return 1;
-    const long long heads = (long long)B * Hkv, all = ceil_div(n_keys, BN);
-    const long long n = (768 + heads - 1) / heads;
-    return (int)max(1LL, min(n, min((all + 3) / 4, 4096LL)));
+// One range for each KV head, which is one launch and no partial sums, where there are few keys (us, one range / the best number of ranges: 8 heads of
+// 768 keys, d = 128, 6.1 / 6.8, of 1024 7.0 / 6.5, of 1536 10.2 / 7.2; 16 of 1024, d = 64, 5.2 / 6.5, of 2048 9.9 / 6.7; 128 of 1024 9.3 / 11.2).
+// Else as many workgroups as there are compute units where all are equally long: a unit has 64 KiB on their way to it in either case, and fewer
+// partial sums (32 heads of 32768 keys, d = 128: 8 ranges 45.0, 12 46.8, 16 49.5, 24 45.7; 128 of 4224: 1 27.0, 2 26.0, 3 27.0, 6 25.8; d = 64, 128 of
+// 32768: 1 119, 2 80, 3 85, 6 83).  Where lengths differ and ranges are dealt out, as many as the units hold at a time, three each, so that what a range is
+// longer than the mean weighs less (128 heads of 200 to 8192 keys: 2 ranges 30.2, 4 29.0, 6 27.8, 8 29.9; 512 of 200 to 2048: 1 29.1, 2 33.2); but
+// one where more than 16 rows make more of the merge: 32 heads of 32 rows of 500 to 8192 keys: 4 ranges 16.9, 8 16.3, 16 19.4, 24 22.9).
+int vfa_kv8_decode_splits(int B, int Hq, int Hkv, int n_q, int d, int n_keys, int varlen) {
+    if (B <= 0 || Hq <= 0 || Hkv <= 0 || n_q <= 0 || n_keys <= 0) return 1;
+    const int n_cu = cu_count() > 0 ? cu_count() : 256, all = ceil_div(n_keys, BN);
+    const long long heads = (long long)B * Hkv, rows = (long long)(Hq / Hkv) * n_q;
+    if (all <= (d == 64 ? 16 : 12)) return 1;
+    const long long n = (varlen && B > 1 && rows <= 16 ? 3 : 1) * (long long)n_cu / heads;
+    return (int)max(1LL, min(n, (all + 3) / 4LL));
 }
 
 size_t vfa_kv8_decode_workspace_bytes(int B, int Hq, int n_q, int d, int n_splits) {
     if (B <= 0 || Hq <= 0 || n_q <= 0 || d <= 0 || n_splits <= 0) return 0;
-    const size_t bytes = (size_t)B * Hq * n_q * n_splits * (2 + (size_t)d) * sizeof(float);
+    const size_t bytes = (size_t)B * Hq * n_q * n_splits * (2 + (size_t)d) * sizeof(float) + 2 * sizeof(int) * (size_t)B;
     return (bytes + 255) & ~(size_t)255;
 }
 
@@ -183,28 +192,44 @@ int vfa_kv8_decode_fwd(const void* Q, const void* K8, const void* V8, const void
     p.g = (int)rows;
     p.c = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)d)) * kLog2e;
     const size_t slots = (size_t)B * Hq * n_q * n_splits;
-    p.opart = (float*)workspace; p.pm = p.opart + slots * d; p.lpart = p.pm + slots;
+    p.opart = (float*)workspace; p.pm = p.opart + slots * d; p.lpart = p.pm + slots; p.dealt = (int*)(p.lpart + slots);
     hipStream_t s = (hipStream_t)stream;
     const int n_cu = cu_count() > 0 ? cu_count() : 256;
     (void)hipGetLastError();
     const long long wgs = (long long)B * Hkv * n_splits;
     if (wgs > kMaxWorkgroups256) return VFA_ERR_UNSUPPORTED;
-    const bool dealt = seq_lens && n_splits > 1 && (B <= 64 || (B <= DEAL_MAX_B && wgs <= 8LL * n_cu && ceil_div(n_cap, BN) > 2 * n_splits));
+    const bool dealt = seq_lens && n_splits > 1 && B > 1 && (B <= 64 || (B <= DEAL_MAX_B && wgs <= 8LL * n_cu && ceil_div(n_cap, BN) > 2 * n_splits));
     with_d(d, [&](auto d_c) {
-        constexpr int D = decltype(d_c)::value, W = 4;
-        auto launch = [&](auto rt_c) {
-            constexpr int RT = decltype(rt_c)::value;
+        constexpr int D = decltype(d_c)::value;
+        // Waves of a workgroup: four have 64 KiB on their way at d = 128, which is what a compute unit gets at a time (one workgroup of 8 waves
+        // takes as long for 2048 keys as one of 4, 13 us); d = 64 has half as much in a wave, and one long range eight waves (32 heads of 2048 keys
+        // 9.9 / 8.2 us, 128 of 32768 119 / 94)
+        const bool wide = D == 64 && n_splits == 1 && p.n_keys > 1024;
+        auto launch = [&](auto rt_c, auto w_c) {
+            constexpr int RT = decltype(rt_c)::value, W = decltype(w_c)::value;
             const dim3 grid((unsigned)n_splits, (unsigned)B, (unsigned)Hkv);
+            if constexpr (W == 8) {
+                if (!seq_lens) kv8_decode_kernel<D, RT, W, LENS_ONE><<<grid, 64 * W, 0, s>>>(P);
+                else kv8_decode_kernel<D, RT, W, LENS_FIXED><<<dim3((unsigned)n_splits, (unsigned)Hkv, (unsigned)B), 64 * W, 0, s>>>(P);
+                return;
+            }
             if (!seq_lens) kv8_decode_kernel<D, RT, W, LENS_ONE><<<grid, 64 * W, 0, s>>>(P);
             else if (dealt) kv8_decode_kernel<D, RT, W, LENS_DEALT><<<grid, 64 * W, 0, s>>>(P);
             else kv8_decode_kernel<D, RT, W, LENS_FIXED><<<dim3((unsigned)n_splits, (unsigned)Hkv, (unsigned)B), 64 * W, 0, s>>>(P);
         };
-        if (rows <= 16) launch(std::integral_constant<int, 1>{});
-        else launch(std::integral_constant<int, 2>{});
+        using std::integral_constant;
+        auto sized = [&](auto w_c) {
+            if (rows <= 16) launch(integral_constant<int, 1>{}, w_c);
+            else launch(integral_constant<int, 2>{}, w_c);
+        };
+        if constexpr (D == 64) {
+            if (wide) sized(integral_constant<int, 8>{});
+        }
+        if (!wide) sized(integral_constant<int, 4>{});
         if (n_splits == 1) return;
         const dim3 grid((unsigned)p.Hq, (unsigned)B);
-        if (dealt) decode_merge_kernel<D, true, true><<<grid, 256, 0, s>>>(p);
-        else decode_merge_kernel<D, false, true><<<grid, 256, 0, s>>>(p);
+        if (dealt) decode_merge_kernel<D, SLOTS_TABLE, true><<<grid, 256, 0, s>>>(p);
+        else decode_merge_kernel<D, SLOTS_FIXED, true><<<grid, 256, 0, s>>>(p);
     });
     return launched();
 }

@@ -725,8 +725,8 @@ int decode_common(const void* Q, const void* K, const void* V, const void* Krepr
             if (!launched) decode_split_kernel<D, W, LENS_FIXED><<<dim3((unsigned)n_splits, (unsigned)Hkv, (unsigned)B), 64 * W, 0, s>>>(p);
         }
         if (n_splits == 1) return;
-        if (dealt) decode_merge_kernel<D, true><<<dim3((unsigned)Hq, (unsigned)B), 256, 0, s>>>(p);
-        else decode_merge_kernel<D, false><<<dim3((unsigned)Hq, (unsigned)B), 256, 0, s>>>(p);
+        if (dealt) decode_merge_kernel<D, SLOTS_SEARCH><<<dim3((unsigned)Hq, (unsigned)B), 256, 0, s>>>(p);
+        else decode_merge_kernel<D, SLOTS_FIXED><<<dim3((unsigned)Hq, (unsigned)B), 256, 0, s>>>(p);
     };
     using std::integral_constant;
     if (single) {

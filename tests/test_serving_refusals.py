@@ -87,10 +87,13 @@ def test_decode(L):
         assert call(f, good, **bad) == INVALID, bad
     for bad in (dict(d=32), dict(cap=127), dict(n_q=9), dict(Hq=66), dict(B=40000), dict(Hq=64, n_q=2)):
         assert call(f, good, **bad) == UNSUPPORTED, bad
-    assert L.vfa_kv8_decode_workspace_bytes(2, 8, 3, 64, 5) == 2 * 8 * 3 * 5 * 66 * 4 + (-(2 * 8 * 3 * 5 * 66 * 4) % 256)
+    assert L.vfa_kv8_decode_workspace_bytes(2, 8, 3, 64, 5) == (2 * 8 * 3 * 5 * 66 * 4 + 16 + 255) // 256 * 256
     assert L.vfa_kv8_decode_workspace_bytes(0, 8, 3, 64, 5) == 0 and L.vfa_kv8_decode_workspace_bytes(1, 8, 0, 64, 5) == 0
     for B, H, n in ((1, 1, 1), (1, 8, 4096), (64, 8, 100000), (1, 1, 1 << 30), (0, 1, 1), (100000, 100000, 1)):
-        assert 1 <= L.vfa_kv8_decode_splits(B, H, n) <= 4096
+        for d in (64, 128):
+            for varlen in (0, 1):
+                assert 1 <= L.vfa_kv8_decode_splits(B, 4 * H, H, 2, d, n, varlen) <= 4096
+    assert L.vfa_kv8_decode_splits(1, 0, 1, 1, 64, 4096, 0) == 1 and L.vfa_kv8_decode_splits(1, 1, 1, 0, 64, 4096, 0) == 1
 
 
 def test_wrappers_refuse_tensors_that_do_not_fit():
