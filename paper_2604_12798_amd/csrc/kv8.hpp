@@ -173,6 +173,81 @@ __global__ __launch_bounds__(2 * D) void kv8_append_kernel(const Kv8Append p) {
     else body(true_type{}, false_type{});
 }
 
+// One new row for each sequence (a decode step): D / 8 lanes hold a row of keys or of values, so a wave has 512 / D rows, of KV heads next to each other, and
+// nothing waits for another wave.  A block that is coded again is done by the whole wave, before the rows are written.
+// (Against a workgroup for each block, 8 KV heads, d = 128, us: 1 sequence 5.6 / 3.0, 16 5.2 / 4.2, 64 7.6 / 3.8; 128 of 16, d = 64, 12.6 / 4.9.)
+template <int D>
+__global__ __launch_bounds__(64) void kv8_append_one_kernel(const Kv8Append p, int rows) {
+    constexpr int G = D / 8;
+    const int lane = threadIdx.x, j = lane % G, f = 8 * j;
+    const int at = blockIdx.x * (64 / G) + lane / G, u = min(at, rows - 1), side = u & 1, bh = u >> 1, b = bh / p.Hkv, h = bh - b * p.Hkv;
+    const int o = min(max(p.old_lens ? p.old_lens[b] : p.old_len, 0), p.n_cap);
+    const bool fresh = at < rows && o < min(p.new_lens ? p.new_lens[b] : p.new_len, p.n_cap);
+    const int tile = min(o / BN, p.T - 1), k = o % BN;
+    const size_t blk = (size_t)bh * p.T + tile;
+    uint8_t* const C = p.C[side] + blk * (BN * D);
+    const u32x4 r = *reinterpret_cast<const u32x4*>(p.X[side] + b * p.sb[side] + h * p.sh[side] + f);
+    const int e_old = (int)p.S[side][blk] - 127;
+    uint32_t a = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const uint32_t lo = r[q] << 16 & 0x7fffffffu, hi = r[q] & 0x7fff0000u;
+        a = max(a, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
+    }
+    auto most = [](uint32_t x, auto ctrl) { return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, 0xf, 0xf, false)); };
+    using std::integral_constant;
+    a = most(a, integral_constant<int, 0xb1>{});   // quad_perm [1, 0, 3, 2], [2, 3, 0, 1], row_half_mirror, row_mirror: over 2, 4, 8, 16 lanes
+    a = most(a, integral_constant<int, 0x4e>{});
+    a = most(a, integral_constant<int, 0x141>{});
+    if (D == 128) a = most(a, integral_constant<int, 0x140>{});
+    int e = kv8_exponent(a);
+    const bool again = fresh && k > 0 && e > e_old;
+    if (k > 0) e = max(e, e_old);
+    uint64_t todo = __builtin_amdgcn_ballot_w64(again && j == 0);
+    if (todo) {
+        do {
+            const int l = __builtin_ctzll(todo);
+            todo &= todo - 1;
+            const int side1 = __builtin_amdgcn_readlane(side, l), k1 = __builtin_amdgcn_readlane(k, l);
+            const uint64_t blk1 = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)blk, l) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(blk >> 32), l) << 32;
+            const float f_old = ldexpf(1.f, __builtin_amdgcn_readlane(e_old, l) - __builtin_amdgcn_readlane(e, l));
+            u32x4* const c = reinterpret_cast<u32x4*>(p.C[side1] + blk1 * (BN * D));
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {  // 16 bytes of a key, or 16 keys of a feature
+                const int n = 64 * i + lane;
+                if (side1 == 0 && (n >> 2) % BN >= k1) continue;
+                u32x4 w = c[n];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const int left = side1 == 0 ? 4 : k1 - (16 * t + 4 * (n & 3));  // old keys of the dword
+                    const uint32_t put = left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << 8 * left) - 1;
+                    float y[4];
+                    kv8_values4(w[t], f_old, y);
+                    w[t] = (w[t] & ~put) | (kv8_codes4(y) & put);
+                }
+                c[n] = w;
+            }
+        } while (todo);
+        __threadfence_block();  // (a row's bytes lie among those that were put back)
+    }
+    if (!fresh) return;
+    const float f_new = ldexpf(1.f, -e);
+    float y[8];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        y[2 * q] = __uint_as_float(r[q] << 16) * f_new;
+        y[2 * q + 1] = __uint_as_float(r[q] & 0xffff0000u) * f_new;
+    }
+    const uint32_t w[2] = {kv8_codes4(y), kv8_codes4(y + 4)};
+    if (side == 0) {
+        *reinterpret_cast<u32x2*>(C + f / 64 * (64 * BN) + k * 64 + f % 64) = u32x2{w[0], w[1]};
+    } else {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) C[(f + q) * BN + kv8_place(k)] = (uint8_t)(w[q >> 2] >> 8 * (q & 3));
+    }
+    if (j == 0) p.S[side][blk] = (uint8_t)(e + 127);
+}
+
 struct Kv8Read {
     const uint8_t* C[2];
     const uint8_t* S[2];

@@ -117,12 +117,19 @@ int vfa_kv8_append(const void* K, const void* V, void* K8, void* V8, void* KS, v
     p.C[0] = (uint8_t*)K8; p.C[1] = (uint8_t*)V8; p.S[0] = (uint8_t*)KS; p.S[1] = (uint8_t*)VS;
     p.old_lens = old_lens; p.new_lens = new_lens; p.old_len = n_old; p.new_len = n_new;
     p.n_in = n_in; p.n_cap = n_cap; p.T = n_cap / BN; p.Hkv = Hkv;
+    (void)hipGetLastError();
+    if (n_in == 1) {
+        const int rows = 2 * B * Hkv, each = 512 / d;
+        with_d(d, [&](auto d_c) {
+            kv8_append_one_kernel<decltype(d_c)::value><<<(unsigned)ceil_div(rows, each), 64, 0, (hipStream_t)stream>>>(p, rows);
+        });
+        return launched();
+    }
     // blocks that the rows can reach, wherever they begin
     const int most = n_in < n_cap ? n_in : n_cap;
     const long long tiles = old_lens ? (most + BN - 2LL) / BN + 1 : (n_new - 1) / BN - n_old / BN + 1;
     if (tiles * 2 * Hkv * B > kMaxWorkgroups256) return VFA_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)tiles, (unsigned)(2 * Hkv), (unsigned)B);
-    (void)hipGetLastError();
     with_d(d, [&](auto d_c) { kv8_append_kernel<decltype(d_c)::value><<<grid, 2 * d, 0, (hipStream_t)stream>>>(p); });
     return launched();
 }

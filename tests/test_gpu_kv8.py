@@ -131,6 +131,29 @@ def test_ragged_batch(vfa, d):
     same_cache(cache, want, [cap] * B)  # everything else is as it was
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("H", [1, 3, 8])
+def test_one_row_each(vfa, d, H):
+    """One new token for each sequence, several times: at a block's beginning, middle and end, none, at the capacity, rows that need a larger scale in
+    some heads only, of keys or of values."""
+    cap = 192
+    old = [0, 1, 3, 62, 63, 64, 100, 127, 128, 191, 192, 50, -4]
+    new = [o + 1 for o in old]
+    new[11], new[6] = 50, 5000
+    B = len(old)
+    o = [min(max(x, 0), cap) for x in old]
+    n = [min(min(y, cap), x + 1) for x, y in zip(o, new)]
+    want = ref.random_cache(B, H, cap, d, 3)
+    cache = ref.pack(want)
+    for i in range(4):
+        K, V = rows((B, H, 1, d), 10 + i), rows((B, H, 1, d), 20 + i)
+        grow = torch.randint(0, 12, (2, B, H, 1, 1), generator=torch.Generator().manual_seed(i))
+        K, V = (K * 2.0 ** grow[0]).to(torch.bfloat16), (V * 2.0 ** grow[1]).to(torch.bfloat16)
+        vfa.kv8_append(K.cuda(), V.cuda(), cache, ints(old), ints(new))
+        want.append(K, V, o, n)
+        same_cache(cache, want, [cap] * B)
+
+
 def test_strides(vfa):
     """Keys and values as slices of one projection, a head axis of stride zero, a batch run backwards through memory."""
     B, H, n, d = 2, 3, 37, 128
