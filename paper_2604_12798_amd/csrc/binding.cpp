@@ -207,6 +207,8 @@ int rows_tensor(PyObject* t, PyObject* dtype, long& device, long long* v, long l
     const Py_ssize_t have = PySequence_Size(s.o);
     if (have != 4) return have < 0 ? -1 : 0;
     if (!entries(s, 4, true, v) || !entries(r, 4, true, st)) return -1;
+    for (int i = 0; i < 3; ++i)
+        if (v[i] <= 1) st[i] = 0;  // (that of an axis of one entry means nothing, and torch lets it be anything)
     return st[3] == 1 || v[3] <= 1;
 }
 PyObject* refused(int ok, const char* what) {

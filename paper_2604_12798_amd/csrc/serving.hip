@@ -190,6 +190,7 @@ int vfa_kv8_decode_fwd(const void* Q, const void* K8, const void* V8, const void
     if ((long long)B * Hq * n_q > 0x7fffffffLL) return VFA_ERR_UNSUPPORTED;
     if (n_splits > 1 && (!workspace || !aligned16(workspace) || workspace_bytes < vfa_kv8_decode_workspace_bytes(B, Hq, n_q, d, n_splits)))
         return VFA_ERR_INVALID_ARG;
+    if (n_cap == 0) n_splits = 1;  // (no keys, so no ranges to deal out)
     Kv8Decode P{};
     DecodeParams& p = P.d;
     P.K8 = (const uint8_t*)K8; P.V8 = (const uint8_t*)V8; P.KS = (const uint8_t*)KS; P.VS = (const uint8_t*)VS;

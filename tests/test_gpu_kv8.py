@@ -171,6 +171,22 @@ def test_strides(vfa):
         same_cache(cache2, want, [n] * B)
 
 
+def test_empty(vfa):
+    """No sequences, no new rows, no capacity."""
+    for B, n, cap in ((0, 3, 64), (2, 0, 64), (2, 0, 0)):
+        cache = vfa.kv8_cache(B, 2, cap, 64)
+        x = torch.zeros((B, 2, n, 64), dtype=torch.bfloat16, device="cuda")
+        vfa.kv8_append(x, x, cache, 0, min(n, cap))
+        vfa.kv8_append(x, x, cache, ints([0] * B), ints([5] * B))
+        assert vfa.kv8_read(cache, 0)[0].shape == (B, 2, 0, 64)
+        q = torch.zeros((B, 4, 3, 64), dtype=torch.bfloat16, device="cuda")
+        for lens in (0, ints([0] * B)):
+            for ns in (None, 1, 4):
+                O, L = vfa.kv8_decode_fwd(q, cache, lens, n_splits=ns)
+                assert (O == 0).all() and L.isneginf().all()
+        assert vfa.kv8_decode_fwd(q[:, :, :0].contiguous(), cache, 0)[0].shape == (B, 4, 0, 64)
+
+
 # ---- reading back ----------------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("d", [64, 128])
@@ -322,6 +338,57 @@ def test_same_bits_again_and_on_another_stream(vfa):
     s.synchronize()
     for x in (second, third):
         assert torch.equal(first[0], x[0]) and torch.equal(first[1], x[1])
+
+
+def test_two_calls_at_once(vfa):
+    """Two streams, a workspace each (the wrapper's own, and given ones), many times."""
+    d, Hq, H, cap = 128, 8, 2, 4096
+    jobs = []
+    for i, (B, n_q, ns) in enumerate(((6, 1, 8), (3, 4, 5))):
+        c = ref.pack(ref.random_cache(B, H, cap, d, 30 + i))
+        q, lens = rows((B, Hq, n_q, d), 40 + i).cuda(), ints([4096 - 600 * b for b in range(B)])
+        ws = torch.empty(vfa.kv8_decode_workspace_bytes(B, Hq, n_q, d, ns), dtype=torch.uint8, device="cuda")
+        jobs.append((q, c, lens, ns, ws, torch.cuda.Stream(), vfa.kv8_decode_fwd(q, c, lens, n_splits=ns)))
+    torch.cuda.synchronize()
+    got = []
+    for i in range(20):
+        for q, c, lens, ns, ws, s, want in jobs:
+            with torch.cuda.stream(s):
+                got.append((want, vfa.kv8_decode_fwd(q, c, lens, n_splits=ns, workspace=ws if i % 2 else None)))
+    torch.cuda.synchronize()
+    for want, x in got:
+        assert torch.equal(want[0], x[0]) and torch.equal(want[1], x[1])
+
+
+def test_refused_tensors(vfa):
+    cache = vfa.kv8_cache(2, 2, 128, 64)
+    x = torch.zeros((2, 2, 3, 64), dtype=torch.bfloat16, device="cuda")
+    q, lens = torch.zeros((2, 4, 64), dtype=torch.bfloat16, device="cuda"), ints([3, 3])
+    bad = [lambda: vfa.kv8_append(x.float(), x, cache, 0, 3), lambda: vfa.kv8_append(x, x.cpu(), cache, 0, 3), lambda: vfa.kv8_append(x[:1], x, cache, 0, 3),
+           lambda: vfa.kv8_append(x, x, cache, lens, 3), lambda: vfa.kv8_append(x, x, cache, lens.long(), lens.long()),
+           lambda: vfa.kv8_append(x, x, cache, lens.cpu(), lens.cpu()), lambda: vfa.kv8_append(x, x, cache[:3] + (cache[3][:1],), 0, 3),
+           lambda: vfa.kv8_append(x, x, cache, lens[:1], lens[:1]), lambda: vfa.kv8_read(cache, 129), lambda: vfa.kv8_read(cache, -1),
+           lambda: vfa.kv8_read(cache, 3, out=(x, x[:, :, :2])), lambda: vfa.kv8_read(cache, 3, seq_lens=lens.float()),
+           lambda: vfa.kv8_decode_fwd(q.float(), cache, 3), lambda: vfa.kv8_decode_fwd(q[:, :, :32], cache, 3), lambda: vfa.kv8_decode_fwd(q[:1], cache, 3),
+           lambda: vfa.kv8_decode_fwd(q, cache, 3, out=x), lambda: vfa.kv8_decode_fwd(q, cache, 3, lse=x), lambda: vfa.kv8_decode_fwd(q, cache, lens.cpu()),
+           lambda: vfa.kv8_decode_fwd(q, cache, 3, n_splits=2, workspace=torch.empty(1 << 16, dtype=torch.uint8)),
+           lambda: vfa.qk_norm_rope_fwd(x, x[:, :, :, ::2]), lambda: vfa.qk_norm_rope_fwd(x, x.cpu()), lambda: vfa.qk_norm_rope_fwd(x, x, x[:1]),
+           lambda: vfa.qk_norm_rope_fwd(x, x, q_weight=q[0, 0].float()), lambda: vfa.qk_norm_rope_fwd(x, x, cos_sin=torch.zeros((4, 64), device="cuda").half()),
+           lambda: vfa.qk_norm_rope_fwd(x, x, cos_sin=torch.zeros(4, device="cuda")), lambda: vfa.qk_norm_rope_fwd(x, x, first_pos=lens.float()),
+           lambda: vfa.qk_norm_rope_fwd(x, x, out=(x, x, None))]
+    for f in bad:
+        with pytest.raises(ValueError):
+            f()
+    codes = [(lambda: vfa.kv8_append(x, x, cache, 0, 4), -1), (lambda: vfa.kv8_append(x, x, cache, 2, 1), -1), (lambda: vfa.kv8_append(x, x, cache, 126, 129), -1),
+             (lambda: vfa.kv8_decode_fwd(q, cache, 129), -1), (lambda: vfa.kv8_decode_fwd(q, cache, 3, n_splits=0), -1),
+             (lambda: vfa.kv8_decode_fwd(q, cache, 3, n_splits=2, workspace=torch.empty(64, dtype=torch.uint8, device="cuda")), -1),
+             (lambda: vfa.kv8_decode_fwd(x.reshape(2, 2, 3, 64).repeat(1, 1, 11, 1).contiguous(), cache, 3), -2),
+             (lambda: vfa.qk_norm_rope_fwd(x, x, eps=-1.0), -1), (lambda: vfa.qk_norm_rope_fwd(x, x, cos_sin=torch.zeros((4, 72), device="cuda")), -1),
+             (lambda: vfa.qk_norm_rope_fwd(x, x, norm=False, q_weight=q[0, 0].contiguous()), -1)]
+    for f, code in codes:
+        with pytest.raises(vfa.VfaError) as e:
+            f()
+        assert e.value.code == code
 
 
 # ---- together --------------------------------------------------------------------------------------------------------------------
