@@ -30,6 +30,16 @@ __device__ __forceinline__ void kv8_values4(uint32_t w, float f, float* y) {
     const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
     y[0] = lo[0] * f; y[1] = lo[1] * f; y[2] = hi[0] * f; y[3] = hi[1] * f;
 }
+// 16 codes of a smaller scale
+__device__ __forceinline__ u32x4 kv8_again(u32x4 w, float f) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        float y[4];
+        kv8_values4(w[q], f, y);
+        w[q] = kv8_codes4(y);
+    }
+    return w;
+}
 // codes 0 and 1 (HI: 2 and 3) of four -> bf16 values times a power of two
 template <typename HI>
 __device__ __forceinline__ uint32_t kv8_bf16x2(uint32_t w, float scale, HI) {
@@ -63,8 +73,11 @@ __device__ __forceinline__ uint32_t wave_umax(uint32_t x) {
 }
 
 // A workgroup of 2 D threads per block that new rows may reach, KV head, keys or values.  Of keys a thread has two runs of 16 features (16 bytes of codes);
-// of values eight features of four neighbouring keys, whose codes are a dword of each feature's row, so that nothing has to be transposed: loads and
-// stores of 16 lanes cover 64 bytes of a row.  A thread is alone with its bytes of the cache; those it does not write it puts back.
+// of values eight features of four neighbouring keys, whose codes are a dword of each feature's row, so that nothing has to be transposed.  Where all tokens of
+// the block are new, and of many, 16 lanes with values cover 64 bytes of a feature's row; of up to 16 tokens 16 lanes (d = 128) cover all features of four, and
+// with keys the waves come one after the other, so that those behind the last have nothing to do (d = 128, us, all lanes spread / this: 1512 blocks with 10 new
+// tokens 15.7 / 12.3, 656 with 3 10.0 / 7.3, 624 with 44 9.5 / 11.9).  A thread is alone with its bytes of the cache; those of a dword that it does not write it
+// puts back.
 template <int D>
 __global__ __launch_bounds__(2 * D) void kv8_append_kernel(const Kv8Append p) {
     __shared__ uint32_t wmax[D / 32];
@@ -78,33 +91,38 @@ __global__ __launch_bounds__(2 * D) void kv8_append_kernel(const Kv8Append p) {
     uint8_t* const C = p.C[side] + blk * (BN * D);
     const uint16_t* const x = p.X[side] + b * p.sb[side] + h * p.sh[side] + (long long)(key0 - o) * p.sn[side];
     const int e_old = (int)p.S[side][blk] - 127;
-    // keys: run u of the thread is features kf to kf + 15 of key kk + 32 u; values: features vf to vf + 7 of keys vk to vk + 3
-    const int kk = threadIdx.x / (D / 16), kf = threadIdx.x % (D / 16) * 16, vk = threadIdx.x % 16 * 4, vf = threadIdx.x / 16 * 8;
-    // (no load sits behind a branch: rows that are not new read a new one again, dwords of values that stay the first that does not)
     auto body = [&](auto side_c, auto whole_c) __attribute__((always_inline)) {
         constexpr bool V = decltype(side_c)::value, WHOLE = decltype(whole_c)::value;  // WHOLE: every token of the block is new
-        uint32_t* const at4 = reinterpret_cast<uint32_t*>(C + vf * BN);
+        const int base = WHOLE ? 0 : V ? k0 & ~3 : k0;  // the first thread's key
+        const int kk = base + threadIdx.x / (D / 16), kf = threadIdx.x % (D / 16) * 16;  // keys: features kf to kf + 15 of keys kk and kk + 32
+        const bool few = !WHOLE && k1 - base <= 16;  // (no more than the first wave's at d = 128)
+        const int vk = few ? base + threadIdx.x / (D / 8) * 4 : threadIdx.x % 16 * 4, vf = few ? threadIdx.x % (D / 8) * 8 : threadIdx.x / 16 * 8;
+        uint32_t* const at4 = reinterpret_cast<uint32_t*>(C + vf * BN);  // values: features vf to vf + 7 of keys vk to vk + 3
+        const int place = kv8_place(vk & (BN - 1)) / 4;
         uint32_t w4[8];
         u32x4 r[4];
+        uint32_t a = 0;
+        // (the lane of a wave's first key decides whether the wave has any; no load sits behind a branch of its own)
+        const bool any = WHOLE || (V && !few) || __builtin_amdgcn_readfirstlane(V ? vk : kk) < k1;
+        if (any) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int key = V ? vk + i : kk + 32 * (i >> 1), f = V ? vf : kf + 8 * (i & 1);
-            r[i] = *reinterpret_cast<const u32x4*>(x + (WHOLE ? key : min(max(key, k0), k1 - 1)) * p.sn[V] + f);
-        }
-        if (V && !WHOLE) {
-            const int near = kv8_place(min(max(vk, k0), k1 - 1) & ~3) / 4;
-#pragma unroll
-            for (int q = 0; q < 8; ++q) w4[q] = at4[q * (BN / 4) + near];
-        }
-        uint32_t a = 0;  // (a new row that is read again does not change the largest)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const uint32_t lo = r[i][q] << 16 & 0x7fffffffu, hi = r[i][q] & 0x7fff0000u;
-                a = max(a, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
+            for (int i = 0; i < 4; ++i) {
+                const int key = V ? vk + i : kk + 32 * (i >> 1), f = V ? vf : kf + 8 * (i & 1);
+                r[i] = *reinterpret_cast<const u32x4*>(x + (WHOLE ? key : min(max(key, k0), k1 - 1)) * p.sn[V] + f);
             }
-        a = wave_umax(a);
+            if (V && !WHOLE)
+#pragma unroll
+                for (int q = 0; q < 8; ++q) w4[q] = at4[q * (BN / 4) + place];
+            // (a new row that is read again does not change the largest)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t lo = r[i][q] << 16 & 0x7fffffffu, hi = r[i][q] & 0x7fff0000u;
+                    a = max(a, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
+                }
+            a = wave_umax(a);
+        }
         if ((threadIdx.x & 63) == 0) wmax[threadIdx.x >> 6] = a;
         __syncthreads();
         a = wmax[0];
@@ -114,38 +132,27 @@ __global__ __launch_bounds__(2 * D) void kv8_append_kernel(const Kv8Append p) {
         const bool again = !WHOLE && k0 > 0 && e > e_old;
         if (!WHOLE && k0 > 0) e = max(e, e_old);
         const float f_new = ldexpf(1.f, -e), f_old = ldexpf(1.f, e_old - e);
-        const int first = again ? 0 : k0;  // keys [first, k1) are written
-        if (!V) {
+        if (threadIdx.x == 0) p.S[V][blk] = (uint8_t)(e + 127);
+        if (any && !V) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const int key = kk + 32 * u;
-                if (!WHOLE && (key < first || key >= k1)) continue;
-                u32x4* const at = reinterpret_cast<u32x4*>(C + kf / 64 * (64 * BN) + key * 64 + kf % 64);
+                if (!WHOLE && key >= k1) continue;
                 float y[16];
-                if (WHOLE || key >= k0) {
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        const uint32_t w = r[2 * u + (q >> 2)][q & 3];
-                        y[2 * q] = __uint_as_float(w << 16) * f_new;
-                        y[2 * q + 1] = __uint_as_float(w & 0xffff0000u) * f_new;
-                    }
-                } else {
-                    const u32x4 w = *at;
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) kv8_values4(w[q], f_old, y + 4 * q);
+                for (int q = 0; q < 8; ++q) {
+                    const uint32_t w = r[2 * u + (q >> 2)][q & 3];
+                    y[2 * q] = __uint_as_float(w << 16) * f_new;
+                    y[2 * q + 1] = __uint_as_float(w & 0xffff0000u) * f_new;
                 }
-                *at = u32x4{kv8_codes4(y), kv8_codes4(y + 4), kv8_codes4(y + 8), kv8_codes4(y + 12)};
+                *reinterpret_cast<u32x4*>(C + kf / 64 * (64 * BN) + key * 64 + kf % 64) = u32x4{kv8_codes4(y), kv8_codes4(y + 4), kv8_codes4(y + 8), kv8_codes4(y + 12)};
             }
-        } else if (WHOLE || (vk < k1 && vk + 4 > first)) {
-            uint32_t put = 0;  // bytes that are written
-            if (!WHOLE) {
+        } else if (any && (WHOLE || (vk < k1 && vk + 4 > k0))) {
+            const int first = again ? 0 : k0;  // keys [first, k1) of the dword are written
+            uint32_t put = 0;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (vk + i >= first && vk + i < k1) put |= 0xffu << 8 * i;
-                if (vk + 4 <= k0)  // (old ones alone, coded again)
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) w4[q] = at4[q * (BN / 4) + kv8_place(vk) / 4];
-            }
+            for (int i = 0; i < 4; ++i)
+                if (vk + i >= first && vk + i < k1) put |= 0xffu << 8 * i;
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
                 float y[4];
@@ -161,9 +168,28 @@ __global__ __launch_bounds__(2 * D) void kv8_append_kernel(const Kv8Append p) {
                 w4[q] = WHOLE ? w : (w4[q] & ~put) | (w & put);
             }
 #pragma unroll
-            for (int q = 0; q < 8; ++q) at4[q * (BN / 4) + kv8_place(vk) / 4] = w4[q];
+            for (int q = 0; q < 8; ++q) at4[q * (BN / 4) + place] = w4[q];
         }
-        if (threadIdx.x == 0) p.S[V][blk] = (uint8_t)(e + 127);
+        if (again) {  // the tokens before, but for those in a dword with a new one
+            const int end = V ? k0 & ~3 : k0;
+            for (int i = threadIdx.x; i < D * BN / 16; i += 2 * D) {
+                if (!V) {
+                    if ((i >> 2) % BN >= end) continue;
+                    u32x4* const at = reinterpret_cast<u32x4*>(C) + i;
+                    *at = kv8_again(*at, f_old);
+                } else {
+                    const int f = i / 4, g = i % 4;  // 16 bytes: the keys 16 t + 4 g + (0..3)
+                    uint32_t* const at = reinterpret_cast<uint32_t*>(C) + f * (BN / 4) + 4 * g;
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        if (16 * t + 4 * g >= end) continue;
+                        float y[4];
+                        kv8_values4(at[t], f_old, y);
+                        at[t] = kv8_codes4(y);
+                    }
+                }
+            }
+        }
     };
     using std::true_type, std::false_type;
     const bool whole = k0 == 0 && k1 == BN;

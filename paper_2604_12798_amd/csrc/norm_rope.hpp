@@ -66,22 +66,26 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(const RopeParams p) {
     const long long tok = (long long)blockIdx.x * ROWS + threadIdx.x / L;
     const bool live = tok < p.tokens;
     const int t = (int)(live ? tok : p.tokens - 1), b = t / p.N, n = t - b * p.N;
-    // chunks of eight features: the two halves of eight pairs, or two neighbours
+    // chunks of eight features: the two halves of eight pairs, or any two; lanes next to each other have chunks next to each other
     const int pairs8 = PAIRS == PAIRS_NONE ? 0 : p.rot / 16;
-    int ca = 2 * j, cb = 2 * j + 1;
-    if (PAIRS == PAIRS_HALF && j < pairs8) { ca = j; cb = j + pairs8; }
-    float cs[8], sn[8];
+    int ca = j, cb = j + L;
+    if (PAIRS == PAIRS_HALF) {
+        ca = j < pairs8 ? j : j + pairs8;
+        cb = j < pairs8 ? j + pairs8 : j + L;
+    }
+    float cs[8], sn[8];  // of the pairs in a chunk of each, or of the eight pairs
     if (PAIRS != PAIRS_NONE) {
         const int pos = (int)min(max((long long)n + (p.first_pos ? p.first_pos[b] : p.first), 0LL), (long long)p.n_pos - 1);
         const float* const c = p.cos_sin + (size_t)pos * p.rot;
-        const int at = j < pairs8 ? 8 * j : 0;
 #pragma unroll
         for (int e4 = 0; e4 < 2; ++e4) {
-            const f32x4 x = *reinterpret_cast<const f32x4*>(c + at + 4 * e4), y = *reinterpret_cast<const f32x4*>(c + p.rot / 2 + at + 4 * e4);
+            const bool turns = PAIRS == PAIRS_HALF ? j < pairs8 : (e4 ? cb : ca) < 2 * pairs8;
+            const int at = !turns ? 0 : PAIRS == PAIRS_HALF ? 8 * j + 4 * e4 : 4 * (e4 ? cb : ca);
+            const f32x4 x = *reinterpret_cast<const f32x4*>(c + at), y = *reinterpret_cast<const f32x4*>(c + p.rot / 2 + at);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                cs[4 * e4 + e] = j < pairs8 ? x[e] : 1.f;
-                sn[4 * e4 + e] = j < pairs8 ? y[e] : 0.f;
+                cs[4 * e4 + e] = turns ? x[e] : 1.f;
+                sn[4 * e4 + e] = turns ? y[e] : 0.f;
             }
         }
     }

@@ -70,10 +70,11 @@ int vfa_qk_norm_rope_fwd(const void* Xq, const void* Xk, const void* Xv, void* Q
     const int rows = 256 / (d / 16);
     const long long wgs = (tokens + rows - 1) / rows;
     // Heads of a thread: four, or one where that gives fewer than two workgroups for each compute unit (16 x 1 tokens of 48 heads: 6.3 / 4.2 us).
-    // Loads and stores past the caches from 256 MiB on (2 x 16384 tokens of 48 heads, 768 MiB, 178 / 164 us; 3 x 777 of 24, d = 64, 14 MiB,
-    // 5.7 / 6.2)
+    // Loads and stores past the caches from 256 MiB on (d = 128, us: 2 x 16384 tokens of 48 heads 178 / 164, 2 x 6240 of 80, neighbouring pairs, 110 / 98;
+    // below 3 x 777 of 24, d = 64, 14 MiB, 5.7 / 6.2), if each covers whole lines of 128 bytes; in parts, a line is fetched twice (7 x 2495 of 96, d = 64, 101 / 128;
+    // 2 x 6240 of 80, half of the features rotated, 112 / 131)
     const int n_cu = cu_count() > 0 ? cu_count() : 256;
-    const bool few = wgs * ((heads + 3) / 4) < 2 * n_cu, stream_past = tokens * heads * d >= 1LL << 26;
+    const bool few = wgs * ((heads + 3) / 4) < 2 * n_cu, stream_past = tokens * heads * d >= 1LL << 26 && d == 128 && (interleaved || rot_dim % 128 == 0);
     const long long ys = few ? heads : (heads + 3) / 4;
     if (ys > 65535 || wgs * ys > kMaxWorkgroups256) return VFA_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)wgs, (unsigned)ys);
