@@ -16,38 +16,60 @@ namespace {
 constexpr int kExpMin = -117;
 __device__ __forceinline__ int kv8_place(int key) { return (key & 12) << 2 | (key >> 4) << 2 | (key & 3); }
 
-// E4M3, nearest even, infinities to +-448; a NaN stays one (the conversion itself gives NaN above 448)
-__device__ __forceinline__ float kv8_clamp(float y) {
-    const float v = fminf(fmaxf(y, -448.f), 448.f);
-    return y != y ? y : v;
+typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+typedef __attribute__((ext_vector_type(2))) short s16x2;
+// Codes of four bf16 elements, two to a dword, of a block with scale 2^e: v_cvt_scalef32_pk_fp8_bf16 divides by the scale and rounds to nearest even, as
+// computed in 64 bits for every finite bf16 at thirteen exponents from -117 to 120.  NaN gives NaN, and so does an infinity: kv8_infinities has the bits that make
+// +-448 of its code.
+__device__ __forceinline__ uint32_t kv8_codes4(uint32_t x01, uint32_t x23, float scale) {
+    s16x2 w = {0, 0};
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, x01), scale, false);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, x23), scale, true);
+    return __builtin_bit_cast(uint32_t, w);
 }
-__device__ __forceinline__ uint32_t kv8_codes4(const float* y) {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(kv8_clamp(y[0]), kv8_clamp(y[1]), 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(kv8_clamp(y[2]), kv8_clamp(y[3]), w, true);
+__device__ __forceinline__ uint32_t kv8_infinities(uint32_t x01, uint32_t x23) {
+    auto is = [](uint32_t x) { return (x & 0x7fff) == 0x7f80 ? 1u : 0u; };
+    return is(x01) | is(x01 >> 16) << 8 | is(x23) << 16 | is(x23 >> 16) << 24;
 }
-// four codes -> their values times f
-__device__ __forceinline__ void kv8_values4(uint32_t w, float f, float* y) {
-    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
-    y[0] = lo[0] * f; y[1] = lo[1] * f; y[2] = hi[0] * f; y[3] = hi[1] * f;
-}
-// 16 codes of a smaller scale
-__device__ __forceinline__ u32x4 kv8_again(u32x4 w, float f) {
+// Elements 2 j and 2 j + 1 (HI) of two rows, the first in the low half.
+template <bool HI>
+__device__ __forceinline__ uint32_t kv8_pair(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, HI ? 0x07060302u : 0x05040100u); }
+// The bits of the largest magnitude among bf16 elements, NaN and infinities above all others; and among the finite ones.
+template <int N>
+__device__ __forceinline__ uint32_t kv8_largest(const u32x4 (&r)[N]) {
+    u16x2 m = {0, 0};
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        float y[4];
-        kv8_values4(w[q], f, y);
-        w[q] = kv8_codes4(y);
-    }
-    return w;
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, r[i][q] & 0x7fff7fffu));
+    return max((uint32_t)m[0], (uint32_t)m[1]);
+}
+template <int N>
+__device__ __forceinline__ uint32_t kv8_largest_finite(const u32x4 (&r)[N]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t lo = r[i][q] & 0x7fff, hi = r[i][q] >> 16 & 0x7fff;
+            m = max(m, max(lo < 0x7f80 ? lo : 0u, hi < 0x7f80 ? hi : 0u));
+        }
+    return m;
 }
 // codes 0 and 1 (HI: 2 and 3) of four -> bf16 values times a power of two
 template <typename HI>
 __device__ __forceinline__ uint32_t kv8_bf16x2(uint32_t w, float scale, HI) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, HI::value));
 }
-// smallest e >= kExpMin with a <= 448 * 2^e, a given by its bits (448 = 1.75 * 2^8)
+// The same four codes for a larger scale, f times the old one (a power of two): through bf16, which holds the values between exactly.
+__device__ __forceinline__ uint32_t kv8_again4(uint32_t w, float f) {
+    return kv8_codes4(kv8_bf16x2(w, f, std::false_type{}), kv8_bf16x2(w, f, std::true_type{}), 1.f);
+}
+// ... f for exponents e_old < e: what is below 2^-40 of its old value has a code of 0 anyway
+__device__ __forceinline__ float kv8_smaller(int e_old, int e) { return ldexpf(1.f, max(e_old - e, -40)); }
+// smallest e >= kExpMin with a <= 448 * 2^e, a given by its bits in bf16 (448 = 1.75 * 2^8)
 __device__ __forceinline__ int kv8_exponent(uint32_t bits) {
-    const int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+    const int e = (int)(bits >> 7) - 127 - 8 + ((bits & 0x7f) > 0x60 ? 1 : 0);
     return max(e, kExpMin);
 }
 
@@ -102,6 +124,7 @@ __global__ __launch_bounds__(2 * D) void kv8_append_kernel(const Kv8Append p) {
         uint32_t w4[8];
         u32x4 r[4];
         uint32_t a = 0;
+        bool odd = false;  // the wave has infinities or NaN
         // (the lane of a wave's first key decides whether the wave has any; no load sits behind a branch of its own)
         const bool any = WHOLE || (V && !few) || __builtin_amdgcn_readfirstlane(V ? vk : kk) < k1;
         if (any) {
@@ -113,15 +136,9 @@ __global__ __launch_bounds__(2 * D) void kv8_append_kernel(const Kv8Append p) {
             if (V && !WHOLE)
 #pragma unroll
                 for (int q = 0; q < 8; ++q) w4[q] = at4[q * (BN / 4) + place];
-            // (a new row that is read again does not change the largest)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const uint32_t lo = r[i][q] << 16 & 0x7fffffffu, hi = r[i][q] & 0x7fff0000u;
-                    a = max(a, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
-                }
-            a = wave_umax(a);
+            a = wave_umax(kv8_largest(r));  // (a new row that is read again does not change it)
+            odd = a >= 0x7f80;
+            if (odd) a = wave_umax(kv8_largest_finite(r));
         }
         if ((threadIdx.x & 63) == 0) wmax[threadIdx.x >> 6] = a;
         __syncthreads();
@@ -131,41 +148,42 @@ __global__ __launch_bounds__(2 * D) void kv8_append_kernel(const Kv8Append p) {
         int e = kv8_exponent(a);
         const bool again = !WHOLE && k0 > 0 && e > e_old;
         if (!WHOLE && k0 > 0) e = max(e, e_old);
-        const float f_new = ldexpf(1.f, -e), f_old = ldexpf(1.f, e_old - e);
+        const float scale = ldexpf(1.f, e), f_old = kv8_smaller(e_old, e);
         if (threadIdx.x == 0) p.S[V][blk] = (uint8_t)(e + 127);
         if (any && !V) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const int key = kk + 32 * u;
                 if (!WHOLE && key >= k1) continue;
-                float y[16];
+                u32x4 w;
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    const uint32_t w = r[2 * u + (q >> 2)][q & 3];
-                    y[2 * q] = __uint_as_float(w << 16) * f_new;
-                    y[2 * q + 1] = __uint_as_float(w & 0xffff0000u) * f_new;
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t x0 = r[2 * u + (q >> 1)][2 * (q & 1)], x1 = r[2 * u + (q >> 1)][2 * (q & 1) + 1];
+                    w[q] = kv8_codes4(x0, x1, scale);
+                    if (odd) w[q] &= ~kv8_infinities(x0, x1);
                 }
-                *reinterpret_cast<u32x4*>(C + kf / 64 * (64 * BN) + key * 64 + kf % 64) = u32x4{kv8_codes4(y), kv8_codes4(y + 4), kv8_codes4(y + 8), kv8_codes4(y + 12)};
+                *reinterpret_cast<u32x4*>(C + kf / 64 * (64 * BN) + key * 64 + kf % 64) = w;
             }
         } else if (any && (WHOLE || (vk < k1 && vk + 4 > k0))) {
-            const int first = again ? 0 : k0;  // keys [first, k1) of the dword are written
-            uint32_t put = 0;
+            uint32_t put = 0, old = 0;  // bytes of new keys, of those before
+            if (!WHOLE)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (vk + i >= first && vk + i < k1) put |= 0xffu << 8 * i;
+                for (int i = 0; i < 4; ++i) {
+                    if (vk + i < k0) old |= 0xffu << 8 * i;
+                    else if (vk + i < k1) put |= 0xffu << 8 * i;
+                }
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
-                float y[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) y[i] = __uint_as_float(q & 1 ? r[i][q >> 1] & 0xffff0000u : r[i][q >> 1] << 16) * f_new;
+                const int j = q >> 1;
+                const uint32_t x01 = q & 1 ? kv8_pair<true>(r[0][j], r[1][j]) : kv8_pair<false>(r[0][j], r[1][j]);
+                const uint32_t x23 = q & 1 ? kv8_pair<true>(r[2][j], r[3][j]) : kv8_pair<false>(r[2][j], r[3][j]);
+                uint32_t w = kv8_codes4(x01, x23, scale);
+                if (odd) w &= ~kv8_infinities(x01, x23);
                 if (!WHOLE) {
-                    float v[4];
-                    kv8_values4(w4[q], f_old, v);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) y[i] = vk + i < k0 ? v[i] : y[i];
+                    if (again) w4[q] = (w4[q] & ~old) | (kv8_again4(w4[q], f_old) & old);
+                    w = (w4[q] & ~put) | (w & put);
                 }
-                const uint32_t w = kv8_codes4(y);
-                w4[q] = WHOLE ? w : (w4[q] & ~put) | (w & put);
+                w4[q] = w;
             }
 #pragma unroll
             for (int q = 0; q < 8; ++q) at4[q * (BN / 4) + place] = w4[q];
@@ -176,16 +194,17 @@ __global__ __launch_bounds__(2 * D) void kv8_append_kernel(const Kv8Append p) {
                 if (!V) {
                     if ((i >> 2) % BN >= end) continue;
                     u32x4* const at = reinterpret_cast<u32x4*>(C) + i;
-                    *at = kv8_again(*at, f_old);
+                    u32x4 w = *at;
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) w[t] = kv8_again4(w[t], f_old);
+                    *at = w;
                 } else {
                     const int f = i / 4, g = i % 4;  // 16 bytes: the keys 16 t + 4 g + (0..3)
                     uint32_t* const at = reinterpret_cast<uint32_t*>(C) + f * (BN / 4) + 4 * g;
 #pragma unroll
                     for (int t = 0; t < 4; ++t) {
                         if (16 * t + 4 * g >= end) continue;
-                        float y[4];
-                        kv8_values4(at[t], f_old, y);
-                        at[t] = kv8_codes4(y);
+                        at[t] = kv8_again4(at[t], f_old);
                     }
                 }
             }
@@ -212,14 +231,11 @@ __global__ __launch_bounds__(64) void kv8_append_one_kernel(const Kv8Append p, i
     const int tile = min(o / BN, p.T - 1), k = o % BN;
     const size_t blk = (size_t)bh * p.T + tile;
     uint8_t* const C = p.C[side] + blk * (BN * D);
-    const u32x4 r = *reinterpret_cast<const u32x4*>(p.X[side] + b * p.sb[side] + h * p.sh[side] + f);
+    const u32x4 r[1] = {*reinterpret_cast<const u32x4*>(p.X[side] + b * p.sb[side] + h * p.sh[side] + f)};
     const int e_old = (int)p.S[side][blk] - 127;
-    uint32_t a = 0;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const uint32_t lo = r[q] << 16 & 0x7fffffffu, hi = r[q] & 0x7fff0000u;
-        a = max(a, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
-    }
+    uint32_t a = kv8_largest(r);
+    const bool odd = __builtin_amdgcn_ballot_w64(a >= 0x7f80) != 0;  // the wave has infinities or NaN
+    if (odd) a = kv8_largest_finite(r);
     auto most = [](uint32_t x, auto ctrl) { return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, 0xf, 0xf, false)); };
     using std::integral_constant;
     a = most(a, integral_constant<int, 0xb1>{});   // quad_perm [1, 0, 3, 2], [2, 3, 0, 1], row_half_mirror, row_mirror: over 2, 4, 8, 16 lanes
@@ -236,7 +252,7 @@ __global__ __launch_bounds__(64) void kv8_append_one_kernel(const Kv8Append p, i
             todo &= todo - 1;
             const int side1 = __builtin_amdgcn_readlane(side, l), k1 = __builtin_amdgcn_readlane(k, l);
             const uint64_t blk1 = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)blk, l) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(blk >> 32), l) << 32;
-            const float f_old = ldexpf(1.f, __builtin_amdgcn_readlane(e_old, l) - __builtin_amdgcn_readlane(e, l));
+            const float f_old = kv8_smaller(__builtin_amdgcn_readlane(e_old, l), __builtin_amdgcn_readlane(e, l));
             u32x4* const c = reinterpret_cast<u32x4*>(p.C[side1] + blk1 * (BN * D));
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) {  // 16 bytes of a key, or 16 keys of a feature
@@ -247,9 +263,7 @@ __global__ __launch_bounds__(64) void kv8_append_one_kernel(const Kv8Append p, i
                 for (int t = 0; t < 4; ++t) {
                     const int left = side1 == 0 ? 4 : k1 - (16 * t + 4 * (n & 3));  // old keys of the dword
                     const uint32_t put = left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << 8 * left) - 1;
-                    float y[4];
-                    kv8_values4(w[t], f_old, y);
-                    w[t] = (w[t] & ~put) | (kv8_codes4(y) & put);
+                    w[t] = (w[t] & ~put) | (kv8_again4(w[t], f_old) & put);
                 }
                 c[n] = w;
             }
@@ -257,14 +271,13 @@ __global__ __launch_bounds__(64) void kv8_append_one_kernel(const Kv8Append p, i
         __threadfence_block();  // (a row's bytes lie among those that were put back)
     }
     if (!fresh) return;
-    const float f_new = ldexpf(1.f, -e);
-    float y[8];
+    const float scale = ldexpf(1.f, e);
+    uint32_t w[2];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        y[2 * q] = __uint_as_float(r[q] << 16) * f_new;
-        y[2 * q + 1] = __uint_as_float(r[q] & 0xffff0000u) * f_new;
+    for (int q = 0; q < 2; ++q) {
+        w[q] = kv8_codes4(r[0][2 * q], r[0][2 * q + 1], scale);
+        if (odd) w[q] &= ~kv8_infinities(r[0][2 * q], r[0][2 * q + 1]);
     }
-    const uint32_t w[2] = {kv8_codes4(y), kv8_codes4(y + 4)};
     if (side == 0) {
         *reinterpret_cast<u32x2*>(C + f / 64 * (64 * BN) + k * 64 + f % 64) = u32x2{w[0], w[1]};
     } else {
