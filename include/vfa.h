@@ -348,8 +348,9 @@ int vfa_mxfp4_attn_noexp_fwd(const void* Q4, const void* QS, const void* K4, con
  *   V8 [B, Hkv, n_cap / 64, d, 64]           codes of values: feature, then token 16 t + 4 g + r of the block at place 16 g + 4 t + r
  *   KS, VS [B, Hkv, n_cap / 64]              the scales' bytes
  * (16-byte aligned codes; n_cap a multiple of 64, else VFA_ERR_UNSUPPORTED; B * Hkv <= 65535).  Nothing of a cache has to be set before its first
- * rows are written.  Rewinding a sequence (drafts that were refused) is a smaller length in the next call.  Lengths are either one for all
- * (ints), or DEVICE arrays of B ints, 4-byte aligned, read by the kernels and clamped to [0, n_cap].  Only d in {64, 128}. ---- */
+ * rows are written.  Rewinding a sequence (drafts that were refused) is a smaller length in the next call.  Lengths are either one for all (ints), or DEVICE
+ * arrays of B ints, 4-byte aligned, read by the kernels and clamped to [0, n_cap].  Only d in {64, 128}.  None of these calls sets a function
+ * attribute: each may be captured first. ---- */
 
 /* Norm, rotation and layout of projected queries, keys and values, one pass.
  *   Xq [B, N, Hq, d], Xk, Xv [B, N, Hkv, d]  bf16, any strides (in elements, multiples of 8: batch, token, head), features contiguous

@@ -217,13 +217,13 @@ int vfa_kv8_decode_fwd(const void* Q, const void* K8, const void* V8, const void
         auto launch = [&](auto rt_c, auto w_c) {
             constexpr int RT = decltype(rt_c)::value, W = decltype(w_c)::value;
             const dim3 grid((unsigned)n_splits, (unsigned)B, (unsigned)Hkv);
-            if constexpr (W == 8) {
-                if (!seq_lens) kv8_decode_kernel<D, RT, W, LENS_ONE><<<grid, 64 * W, 0, s>>>(P);
-                else kv8_decode_kernel<D, RT, W, LENS_FIXED><<<dim3((unsigned)n_splits, (unsigned)Hkv, (unsigned)B), 64 * W, 0, s>>>(P);
-                return;
+            if constexpr (W == 4) {  // (one range is not dealt out)
+                if (dealt) {
+                    kv8_decode_kernel<D, RT, W, LENS_DEALT><<<grid, 64 * W, 0, s>>>(P);
+                    return;
+                }
             }
             if (!seq_lens) kv8_decode_kernel<D, RT, W, LENS_ONE><<<grid, 64 * W, 0, s>>>(P);
-            else if (dealt) kv8_decode_kernel<D, RT, W, LENS_DEALT><<<grid, 64 * W, 0, s>>>(P);
             else kv8_decode_kernel<D, RT, W, LENS_FIXED><<<dim3((unsigned)n_splits, (unsigned)Hkv, (unsigned)B), 64 * W, 0, s>>>(P);
         };
         using std::integral_constant;
