@@ -103,16 +103,19 @@ __device__ __forceinline__ uint32_t wave_umax(uint32_t x) {
 template <int D>
 __global__ __launch_bounds__(2 * D) void kv8_append_kernel(const Kv8Append p) {
     __shared__ uint32_t wmax[D / 32];
+    __shared__ int was;
     const int side = blockIdx.y & 1, h = blockIdx.y >> 1, b = blockIdx.z;
     const int o = min(max(p.old_lens ? p.old_lens[b] : p.old_len, 0), p.n_cap);
-    const int n = min(min(p.new_lens ? p.new_lens[b] : p.new_len, p.n_cap), o + p.n_in);
-    const int tile = o / BN + blockIdx.x, key0 = tile * BN;
-    if (o >= n || key0 >= n) return;
+    const int end = min(max(p.new_lens ? p.new_lens[b] : p.new_len, 0), p.n_cap), n = end - o > p.n_in ? o + p.n_in : end;
+    const int tile = o / BN + blockIdx.x;
+    if (o >= n || tile > (n - 1) / BN) return;
+    const int key0 = tile * BN;
     const int k0 = max(o - key0, 0), k1 = min(n - key0, BN);  // the block's new rows
     const size_t blk = ((size_t)b * p.Hkv + h) * p.T + tile;
     uint8_t* const C = p.C[side] + blk * (BN * D);
     const uint16_t* const x = p.X[side] + b * p.sb[side] + h * p.sh[side] + (long long)(key0 - o) * p.sn[side];
-    const int e_old = (int)p.S[side][blk] - 127;
+    // (one thread reads the old exponent and writes the new one, whoever else may be late)
+    if (threadIdx.x == 0) was = (int)p.S[side][blk] - 127;
     auto body = [&](auto side_c, auto whole_c) __attribute__((always_inline)) {
         constexpr bool V = decltype(side_c)::value, WHOLE = decltype(whole_c)::value;  // WHOLE: every token of the block is new
         const int base = WHOLE ? 0 : V ? k0 & ~3 : k0;  // the first thread's key
@@ -146,6 +149,7 @@ __global__ __launch_bounds__(2 * D) void kv8_append_kernel(const Kv8Append p) {
 #pragma unroll
         for (int w = 1; w < D / 32; ++w) a = max(a, wmax[w]);
         int e = kv8_exponent(a);
+        const int e_old = was;
         const bool again = !WHOLE && k0 > 0 && e > e_old;
         if (!WHOLE && k0 > 0) e = max(e, e_old);
         const float scale = ldexpf(1.f, e), f_old = kv8_smaller(e_old, e);

@@ -171,6 +171,20 @@ def test_strides(vfa):
         same_cache(cache2, want, [n] * B)
 
 
+def test_more_rows_than_fit(vfa):
+    """As many rows as an int counts (all of them one row), of which few are taken; lengths at the ends of their type."""
+    B, H, cap, d = 5, 2, 192, 64
+    old, new = [100, 0, 191, 2 ** 31 - 1, -2 ** 31], [101, 2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1, -2 ** 31]
+    one = rows((B, H, 1, d), 6)
+    x = one.cuda().expand(B, H, 2 ** 31 - 1, d)
+    want = ref.random_cache(B, H, cap, d, 5)
+    cache = ref.pack(want)
+    vfa.kv8_append(x, x, cache, ints(old), ints(new))
+    few = one.expand(B, H, cap, d)
+    want.append(few, few, [100, 0, 191, 192, 0], [101, 192, 192, 192, 0])
+    same_cache(cache, want, [cap] * B)
+
+
 def test_empty(vfa):
     """No sequences, no new rows, no capacity."""
     for B, n, cap in ((0, 3, 64), (2, 0, 64), (2, 0, 0)):
@@ -263,6 +277,19 @@ def test_many_sequences(vfa, B, n_splits):
 def test_scale_and_large_scores(vfa):
     run_decode(vfa, 2, 4, 2, 256, 128, 1, [256, 100], 2, softmax_scale=0.5)
     run_decode(vfa, 2, 4, 2, 256, 128, 2, [256, 100], 2, q_size=20.0)
+
+
+@pytest.mark.parametrize("up", [-90, -30, 30, 80])
+def test_scales_of_any_size(vfa, up):
+    """Keys 2^up times as large under a softmax scale as much smaller, and values 2^up times as large, bit for bit."""
+    B, H, cap, d = 3, 2, 320, 128
+    lens = ints([320, 63, 130])
+    q = rows((B, 8, 2, d), 2, 0.4).cuda()
+    c = ref.random_cache(B, H, cap, d, 1)
+    O, L = vfa.kv8_decode_fwd(q, ref.pack(c), lens, n_splits=2, softmax_scale=2.0 ** -4)
+    c.exp = [e + up for e in c.exp]
+    O2, L2 = vfa.kv8_decode_fwd(q, ref.pack(c), lens, n_splits=2, softmax_scale=2.0 ** (-4 - up))
+    assert torch.equal(L, L2) and torch.equal(O.double() * 2.0 ** up, O2.double())
 
 
 def test_nothing_behind_the_end_is_seen(vfa):
