@@ -454,7 +454,7 @@ def mxfp4_attn_fwd(Q4, QS, K4, KS, Vt8, *, descale_v, frozen=True, block_m=128, 
     return O, L, ws
 
 
-_empty_like = _f32 = _u8 = _tensor = None
+_empty_like = _f32 = _u8 = None
 
 
 def _serving(device):
@@ -465,21 +465,12 @@ def _serving(device):
 
 def _ns():
     """_n(), and what the wrappers of the serving operators use of torch on every call."""
-    global _empty_like, _f32, _u8, _tensor, _current_device, _current_stream
+    global _empty_like, _f32, _u8, _current_device, _current_stream
     if _empty_like is None:
         import torch
-        _empty_like, _f32, _u8, _tensor = torch.empty_like, torch.float32, torch.uint8, torch.Tensor
+        _empty_like, _f32, _u8 = torch.empty_like, torch.float32, torch.uint8
         _current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
     return _native or _n()
-
-
-def _lengths(x, n, B, device, what):
-    """(device array or None, whole number) of lengths that are one for all or an int32 tensor of B entries."""
-    if not isinstance(x, _tensor):
-        return None, int(x)
-    if not n.check_tensor(x, _i32, device, B):
-        raise ValueError(f"{what} must be a whole number or a contiguous int32 tensor of {B} entries on the same GPU")
-    return x, 0
 
 
 def _need(ok, what):
@@ -494,16 +485,8 @@ def qk_norm_rope_fwd(q, k, v=None, *, norm=True, q_weight=None, k_weight=None, e
     rotated by position (cos_sin [n_pos, rot] fp32: cosines, then sines; None: no rotation).  first_pos: position of token 0, a
     number or an int32 tensor of B entries.  out: (Q, K, V) to write to."""
     n = _ns()
-    dev, B, N, Hq, Hkv, d, *strides = n.check_norm_rope(q, k, v, _bf16)
+    dev, B, N, Hq, Hkv, d, *strides, n_pos, rot, at, first = n.check_norm_rope(q, k, v, q_weight, k_weight, cos_sin, first_pos, _bf16, _f32, _i32)
     _serving(dev)
-    for w in (q_weight, k_weight):
-        _need(w is None or n.check_tensor(w, _bf16, dev, d), "weights must be contiguous bf16 tensors of d entries on the same GPU")
-    n_pos = rot = 0
-    if cos_sin is not None:
-        _need(cos_sin.dim() == 2, "cos_sin must be a contiguous fp32 tensor [n_pos, rot] on the same GPU")
-        n_pos, rot = cos_sin.shape
-        _need(n.check_tensor(cos_sin, _f32, dev, n_pos, rot), "cos_sin must be a contiguous fp32 tensor [n_pos, rot] on the same GPU")
-    at, first = _lengths(first_pos, n, B, dev, "first_pos")
     if out is None:
         Q, K = q.new_empty((B, Hq, N, d)), q.new_empty((B, Hkv, N, d))
         V = None if v is None else _empty_like(K)
@@ -534,11 +517,9 @@ def kv8_append(K, V, cache, old_lens, new_lens, stream=None):
     sequence (numbers, or int32 tensors of B entries, both alike)."""
     n = _ns()
     K8, V8, KS, VS = cache
-    dev, B, Hkv, n_cap, n_in, d, *strides = n.check_kv8_append(K, V, K8, V8, KS, VS, _bf16, _u8)
+    dev, *sizes = n.check_kv8_append(K, V, K8, V8, KS, VS, old_lens, new_lens, _bf16, _u8, _i32)
     _serving(dev)
-    (o, n_old), (m, n_new) = _lengths(old_lens, n, B, dev, "old_lens"), _lengths(new_lens, n, B, dev, "new_lens")
-    _need((o is None) == (m is None), "old_lens and new_lens must both be numbers or both be tensors")
-    rc = n.vfa_kv8_append_t(K, V, K8, V8, KS, VS, B, Hkv, n_cap, n_in, d, *strides, o, m, n_old, n_new, _stream(stream))
+    rc = n.vfa_kv8_append_t(K, V, K8, V8, KS, VS, *sizes, _stream(stream))
     if rc != 0:
         raise VfaError(rc, "vfa_kv8_append")
     return cache
@@ -549,11 +530,10 @@ def kv8_read(cache, n: int, *, seq_lens=None, out=None, stream=None):
     entries; None: n)."""
     nat = _ns()
     K8, V8, KS, VS = cache
-    dev, B, Hkv, n_cap, d = nat.check_cache8(K8, V8, KS, VS, _u8)
-    _serving(dev)
     n = int(n)
+    dev, B, Hkv, n_cap, d, lens, length = nat.check_cache8(K8, V8, KS, VS, n if seq_lens is None else seq_lens, _u8, _i32)
+    _serving(dev)
     _need(0 <= n <= n_cap, f"n must be between 0 and the cache's {n_cap} tokens")
-    lens, length = _lengths(n if seq_lens is None else seq_lens, nat, B, dev, "seq_lens")
     if out is None:
         K = K8.new_empty((B, Hkv, n, d), dtype=_bf16)
         V = _empty_like(K)
@@ -582,9 +562,8 @@ def kv8_decode_fwd(q, cache, seq_lens, *, n_splits=None, softmax_scale=0.0, work
     lengths are on the GPU).  A workspace of kv8_decode_workspace_bytes is for calls that must not allocate."""
     n = _ns()
     K8, V8, KS, VS = cache
-    dev, B, Hq, Hkv, n_cap, n_q, d = n.check_kv8_decode(q, K8, V8, KS, VS, _bf16, _u8)
+    dev, B, Hq, Hkv, n_cap, n_q, d, lens, n_keys = n.check_kv8_decode(q, K8, V8, KS, VS, seq_lens, _bf16, _u8, _i32)
     _serving(dev)
-    lens, n_keys = _lengths(seq_lens, n, B, dev, "seq_lens")
     if n_splits is None:
         n_splits = n.vfa_kv8_decode_splits(B, Hq, Hkv, n_q, d, n_keys if lens is None else n_cap, int(lens is not None))
     n_splits = int(n_splits)
@@ -595,7 +574,7 @@ def kv8_decode_fwd(q, cache, seq_lens, *, n_splits=None, softmax_scale=0.0, work
     if lse is not None:
         _need(n.check_tensor(lse, _f32, dev, *q.shape[:-1]), "lse must be a contiguous fp32 tensor of q's shape without d on the same GPU")
     elif want_lse:
-        lse = q.new_empty(q.shape[:-1], dtype=_f32)
+        lse = q.new_empty((B, Hq, n_q) if q.dim() == 4 else (B, Hq), dtype=_f32)
     ws_bytes = 0
     if n_splits > 1:
         if workspace is None:

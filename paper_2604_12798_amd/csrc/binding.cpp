@@ -211,6 +211,31 @@ int rows_tensor(PyObject* t, PyObject* dtype, long& device, long long* v, long l
         if (v[i] <= 1) st[i] = 0;  // (that of an axis of one entry means nothing, and torch lets it be anything)
     return st[3] == 1 || v[3] <= 1;
 }
+// Lengths or positions that are one number for all, or a contiguous int32 tensor of B entries on `device`: the tensor (or None) and the number (0).
+// 1, 0 (refused), or -1 with an error set
+struct Lengths {
+    PyObject *at = nullptr, *number = nullptr;  // (new references)
+    ~Lengths() { Py_XDECREF(at); Py_XDECREF(number); }
+    Lengths() = default;
+    Lengths(const Lengths&) = delete;
+    Lengths& operator=(const Lengths&) = delete;
+    int set(PyObject* x, PyObject* int32, long device, long long B) {
+        if (!PyLong_Check(x) && PyObject_HasAttr(x, names.get_device)) {
+            long long n[1];
+            const int ok = whole_tensor(x, int32, device, 1, n);
+            if (ok != 1 || n[0] != B) return ok == 1 ? 0 : ok;
+            Py_INCREF(x);
+            at = x;
+            number = PyLong_FromLong(0);
+        } else {
+            Py_INCREF(Py_None);
+            at = Py_None;
+            number = PyNumber_Long(x);
+        }
+        return number ? 1 : -1;
+    }
+};
+const char kLengths[] = "lengths and positions are numbers, or contiguous int32 tensors of an entry for each sequence on the same GPU";
 PyObject* refused(int ok, const char* what) {
     if (ok == 0) PyErr_SetString(PyExc_ValueError, what);
     return nullptr;
@@ -230,59 +255,84 @@ int cache8(PyObject* const* c, PyObject* uint8, long& device, long long* v) {
 }
 const char kCache8[] = "a cache is four contiguous uint8 tensors on one GPU: K8 [B, Hkv, T, d / 64, 64, 64], V8 [B, Hkv, T, d, 64], KS and VS [B, Hkv, T]";
 
-// check_cache8(K8, V8, KS, VS, uint8) -> (device, B, Hkv, n_cap, d)
+// check_cache8(K8, V8, KS, VS, lengths, uint8, int32) -> (device, B, Hkv, n_cap, d, seq_lens, seq_len)
 PyObject* check_cache8(PyObject*, PyObject* const* args, Py_ssize_t n) {
-    if (n != 5) return PyErr_Format(PyExc_TypeError, "expected 5 arguments, got %zd", n);
-    long device = -1;
-    long long c[4];
-    const int ok = cache8(args, args[4], device, c);
-    if (ok != 1) return refused(ok, kCache8);
-    return Py_BuildValue("(lLLLL)", device, c[0], c[1], 64 * c[2], 64 * c[3]);
-}
-// check_kv8_append(K, V, K8, V8, KS, VS, bfloat16, uint8) -> (device, B, Hkv, n_cap, n_in, d, strides of K, strides of V)
-PyObject* check_kv8_append(PyObject*, PyObject* const* args, Py_ssize_t n) {
-    if (n != 8) return PyErr_Format(PyExc_TypeError, "expected 8 arguments, got %zd", n);
-    long device = -1;
-    long long c[4], k[4], v[4], ks[4], vs[4];
-    int ok = cache8(args + 2, args[7], device, c);
-    if (ok != 1) return refused(ok, kCache8);
-    ok = rows_tensor(args[0], args[6], device, k, ks);
-    if (ok == 1) ok = rows_tensor(args[1], args[6], device, v, vs);
-    if (ok == 1) ok = k[0] == c[0] && k[1] == c[1] && k[3] == 64 * c[3] && v[0] == k[0] && v[1] == k[1] && v[2] == k[2] && v[3] == k[3];
-    if (ok != 1) return refused(ok, "K, V must be bf16 tensors [B, Hkv, n_in, d] matching the cache and on its GPU, their last dimension contiguous");
-    return Py_BuildValue("(lLLLLLLLLLLL)", device, c[0], c[1], 64 * c[2], k[2], 64 * c[3], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2]);
-}
-// check_kv8_decode(q, K8, V8, KS, VS, bfloat16, uint8) -> (device, B, Hq, Hkv, n_cap, n_q, d)
-PyObject* check_kv8_decode(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (n != 7) return PyErr_Format(PyExc_TypeError, "expected 7 arguments, got %zd", n);
     long device = -1;
+    long long c[4];
+    int ok = cache8(args, args[5], device, c);
+    if (ok != 1) return refused(ok, kCache8);
+    Lengths l;
+    ok = l.set(args[4], args[6], device, c[0]);
+    if (ok != 1) return refused(ok, kLengths);
+    return Py_BuildValue("(lLLLLOO)", device, c[0], c[1], 64 * c[2], 64 * c[3], l.at, l.number);
+}
+// check_kv8_append(K, V, K8, V8, KS, VS, old, new, bfloat16, uint8, int32) -> (device, B, Hkv, n_cap, n_in, d, strides of K, strides of V,
+// old_lens, new_lens, n_old, n_new)
+PyObject* check_kv8_append(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 11) return PyErr_Format(PyExc_TypeError, "expected 11 arguments, got %zd", n);
+    long device = -1;
+    long long c[4], k[4], v[4], ks[4], vs[4];
+    int ok = cache8(args + 2, args[9], device, c);
+    if (ok != 1) return refused(ok, kCache8);
+    ok = rows_tensor(args[0], args[8], device, k, ks);
+    if (ok == 1) ok = rows_tensor(args[1], args[8], device, v, vs);
+    if (ok == 1) ok = k[0] == c[0] && k[1] == c[1] && k[3] == 64 * c[3] && v[0] == k[0] && v[1] == k[1] && v[2] == k[2] && v[3] == k[3];
+    if (ok != 1) return refused(ok, "K, V must be bf16 tensors [B, Hkv, n_in, d] matching the cache and on its GPU, their last dimension contiguous");
+    Lengths o, m;
+    ok = o.set(args[6], args[10], device, c[0]);
+    if (ok == 1) ok = m.set(args[7], args[10], device, c[0]);
+    if (ok == 1) ok = (o.at == Py_None) == (m.at == Py_None);
+    if (ok != 1) return refused(ok, "old_lens and new_lens are both numbers, or both contiguous int32 tensors of an entry for each sequence on the same GPU");
+    return Py_BuildValue("(lLLLLLLLLLLLOOOO)", device, c[0], c[1], 64 * c[2], k[2], 64 * c[3], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], o.at, m.at, o.number,
+                         m.number);
+}
+// check_kv8_decode(q, K8, V8, KS, VS, lengths, bfloat16, uint8, int32) -> (device, B, Hq, Hkv, n_cap, n_q, d, seq_lens, n_keys)
+PyObject* check_kv8_decode(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 9) return PyErr_Format(PyExc_TypeError, "expected 9 arguments, got %zd", n);
+    long device = -1;
     long long c[4], q[4] = {0, 0, 1, 0};
-    int ok = cache8(args + 1, args[6], device, c);
+    int ok = cache8(args + 1, args[7], device, c);
     if (ok != 1) return refused(ok, kCache8);
     const Ref dims = method(args[0], names.dim);
     const long nd = dims.o ? PyLong_AsLong(dims.o) : -1;
     if (nd == -1 && PyErr_Occurred()) return nullptr;
     ok = nd == 3 || nd == 4;
-    if (ok == 1) ok = whole_tensor(args[0], args[5], device, nd, q);
+    if (ok == 1) ok = whole_tensor(args[0], args[6], device, nd, q);
     if (ok == 1 && nd == 3) { q[3] = q[2]; q[2] = 1; }
     if (ok == 1) ok = q[0] == c[0] && q[3] == 64 * c[3];
     if (ok != 1) return refused(ok, "q must be a contiguous bf16 tensor [B, Hq, n_q, d] or [B, Hq, d] matching the cache and on its GPU");
-    return Py_BuildValue("(lLLLLLL)", device, c[0], q[1], c[1], 64 * c[2], q[2], q[3]);
+    Lengths l;
+    ok = l.set(args[5], args[8], device, c[0]);
+    if (ok != 1) return refused(ok, kLengths);
+    return Py_BuildValue("(lLLLLLLOO)", device, c[0], q[1], c[1], 64 * c[2], q[2], q[3], l.at, l.number);
 }
-// check_norm_rope(q, k, v or None, bfloat16) -> (device, B, N, Hq, Hkv, d, strides of q, of k, of v)
+// check_norm_rope(q, k, v or None, q_weight or None, k_weight or None, cos_sin or None, position, bfloat16, float32, int32) -> (device, B, N, Hq, Hkv, d,
+// strides of q, of k, of v, n_pos, rot, first_pos, first)
 PyObject* check_norm_rope(PyObject*, PyObject* const* args, Py_ssize_t n) {
-    if (n != 4) return PyErr_Format(PyExc_TypeError, "expected 4 arguments, got %zd", n);
+    if (n != 10) return PyErr_Format(PyExc_TypeError, "expected 10 arguments, got %zd", n);
     long device = -1;
-    long long q[4], k[4], v[4], qs[4], ks[4], vs[4] = {0, 0, 0, 0};
-    int ok = rows_tensor(args[0], args[3], device, q, qs);
-    if (ok == 1) ok = rows_tensor(args[1], args[3], device, k, ks);
+    long long q[4], k[4], v[4], qs[4], ks[4], vs[4] = {0, 0, 0, 0}, w[1], table[2] = {0, 0};
+    int ok = rows_tensor(args[0], args[7], device, q, qs);
+    if (ok == 1) ok = rows_tensor(args[1], args[7], device, k, ks);
     if (ok == 1) ok = k[0] == q[0] && k[1] == q[1] && k[3] == q[3];
     if (ok == 1 && args[2] != Py_None) {
-        ok = rows_tensor(args[2], args[3], device, v, vs);
+        ok = rows_tensor(args[2], args[7], device, v, vs);
         if (ok == 1) ok = v[0] == k[0] && v[1] == k[1] && v[2] == k[2] && v[3] == k[3];
     }
     if (ok != 1) return refused(ok, "q [B, N, Hq, d], k and v [B, N, Hkv, d] must be bf16 tensors on one GPU, their last dimension contiguous");
-    return Py_BuildValue("(lLLLLLLLLLLLLLL)", device, q[0], q[1], q[2], k[2], q[3], qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2]);
+    for (int i = 3; i < 5; ++i) {
+        if (args[i] != Py_None) ok = whole_tensor(args[i], args[7], device, 1, w);
+        if (ok == 1 && args[i] != Py_None) ok = w[0] == q[3];
+        if (ok != 1) return refused(ok, "weights are contiguous bf16 tensors of d entries on the same GPU");
+    }
+    if (args[5] != Py_None) ok = whole_tensor(args[5], args[8], device, 2, table);
+    if (ok != 1) return refused(ok, "cos_sin is a contiguous fp32 tensor [n_pos, rot] on the same GPU");
+    Lengths first;
+    ok = first.set(args[6], args[9], device, q[0]);
+    if (ok != 1) return refused(ok, kLengths);
+    return Py_BuildValue("(lLLLLLLLLLLLLLLLLOO)", device, q[0], q[1], q[2], k[2], q[3], qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], table[0],
+                         table[1], first.at, first.number);
 }
 // check_tensor(t, dtype, device, shape...): a contiguous tensor of that kind
 PyObject* check_tensor(PyObject*, PyObject* const* args, Py_ssize_t n) {

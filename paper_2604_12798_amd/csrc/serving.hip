@@ -159,14 +159,16 @@ int vfa_kv8_read(const void* K8, const void* V8, const void* KS, const void* VS,
 // Else as many workgroups as there are compute units where all are equally long: a unit has 64 KiB on their way to it in either case, and fewer
 // partial sums (32 heads of 32768 keys, d = 128: 8 ranges 45.0, 12 46.8, 16 49.5, 24 45.7; 128 of 4224: 1 27.0, 2 26.0, 3 27.0, 6 25.8; d = 64, 128 of
 // 32768: 1 119, 2 80, 3 85, 6 83).  Where lengths differ and ranges are dealt out, as many as the units hold at a time, three each, so that what a range is
-// longer than the mean weighs less (128 heads of 200 to 8192 keys: 2 ranges 30.2, 4 29.0, 6 27.8, 8 29.9; 512 of 200 to 2048: 1 29.1, 2 33.2); but
+// longer than the mean weighs less (128 heads of 200 to 8192 keys: 2 ranges 30.2, 4 29.0, 6 27.8, 8 29.9; 512 of 200 to 2048: 1 29.1, 2 33.2; more fit
+// in at d = 64, 288 heads of 300 to 6175 keys: 2 30.2, 3 26.9, 4 26.8); but
 // one where more than 16 rows make more of the merge: 32 heads of 32 rows of 500 to 8192 keys: 4 ranges 16.9, 8 16.3, 16 19.4, 24 22.9).
 int vfa_kv8_decode_splits(int B, int Hq, int Hkv, int n_q, int d, int n_keys, int varlen) {
     if (B <= 0 || Hq <= 0 || Hkv <= 0 || n_q <= 0 || n_keys <= 0) return 1;
     const int n_cu = cu_count() > 0 ? cu_count() : 256, all = ceil_div(n_keys, BN);
     const long long heads = (long long)B * Hkv, rows = (long long)(Hq / Hkv) * n_q;
     if (all <= (d == 64 ? 16 : 12)) return 1;
-    const long long n = (varlen && B > 1 && rows <= 16 ? 3 : 1) * (long long)n_cu / heads;
+    const bool dealt = varlen && B > 1 && rows <= 16;
+    const long long n = (dealt ? 3LL * n_cu + (d == 64 ? heads - 1 : 0) : (long long)n_cu) / heads;
     return (int)max(1LL, min(n, (all + 3) / 4LL));
 }
 
