@@ -268,7 +268,7 @@ def test_one_length_for_all(vfa, n, n_splits):
     run_decode(vfa, 2, 8, 2, 1024, 64, 3, [n, n], n_splits, uniform=True, seed=n)
 
 
-@pytest.mark.parametrize("B,n_splits", [(70, 2), (256, 3), (300, 2), (300, 1)])
+@pytest.mark.parametrize("B,n_splits", [(70, 2), (256, 3), (300, 2), (300, 1), (5000, None)])
 def test_many_sequences(vfa, B, n_splits):
     """Batches whose ranges are dealt out, and batches above that."""
     run_decode(vfa, B, 4, 1, 320, 64, 1, [(37 * b) % 321 for b in range(B)], n_splits, seed=B)
