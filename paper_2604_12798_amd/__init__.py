@@ -557,8 +557,8 @@ def kv8_decode_splits(B: int, Hq: int, Hkv: int, n_q: int, d: int, n_keys: int, 
 
 
 def kv8_decode_fwd(q, cache, seq_lens, *, n_splits=None, softmax_scale=0.0, workspace=None, out=None, lse=None, want_lse=True, stream=None):
-    """Attention of each sequence's newest tokens, q [B, Hq, n_q, d] (or [B, Hq, d] for one), over the cache that holds them already;
-    seq_lens: a number or an int32 tensor of B entries.  n_splits: key ranges (None: vfa_kv8_decode_splits, of the cache's capacity where the
+    """Attention of each sequence's newest tokens, q [B, Hq, n_q, d] (or [B, Hq, d] for one), over the cache that holds them already: a step, drafts,
+    a piece of a prompt; seq_lens: a number or an int32 tensor of B entries.  n_splits: key ranges (None: vfa_kv8_decode_splits, of the cache's capacity where the
     lengths are on the GPU).  A workspace of kv8_decode_workspace_bytes is for calls that must not allocate."""
     n = _ns()
     K8, V8, KS, VS = cache

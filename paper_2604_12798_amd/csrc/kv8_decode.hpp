@@ -17,6 +17,10 @@ namespace {
 // Token t of the n_q sees keys < len - n_q + 1 + t.  What lies behind a sequence's end is neither a key (its scores are -inf) nor a value (its
 // codes are cleared: 0 * NaN).  A NaN in the value of a key that only some of the tokens see would reach the others through weights of zero: it is
 // cleared, too, and the sums of those who see it are set.
+// More than 32 rows (GROUPED: a prompt in pieces) are cut into groups of as many tokens as give 32, each with a workgroup of its own for each range; its last
+// token's keys take the place of the sequence's.  The groups of a KV head, next to each other in the grid, find its tiles in L2, so their loads are not
+// non-temporal, and the matrix unit is what bounds them: the last 1024 of 16384 tokens of 32 heads over 8, D = 128, 308 us (864 TFLOP/s), all of 2 x 16384
+// 4.51 ms (976), 64 of 16384 46 us.  (The scores cost as many conversions for 32 rows as for one.)
 // Partial sums of ranges and their merge: decode.hpp, a row for a head.
 struct Kv8Decode {
     DecodeParams d;  // Hq, g: rows for heads (query heads times new tokens); K, V not used
@@ -25,6 +29,7 @@ struct Kv8Decode {
     const uint8_t* KS;
     const uint8_t* VS;
     int T, n_q;
+    int g, tokens, groups;  // GROUPED: query heads per KV head; tokens of a workgroup (their rows at most 32); groups of so many
 };
 
 // eight codes -> bf16 values
@@ -42,14 +47,14 @@ __device__ __forceinline__ float kg_sum(float x) {
     return xhalf_sum(__uint_as_float(a[0]) + __uint_as_float(a[1]));
 }
 // A block's codes: bytes 1024 u + off of it, u = 0..NI - 1; with `bytes` = 0 zeros, and no access.
-template <int NI>
+template <int NI, bool NT>
 __device__ __forceinline__ void kv8_request(const uint8_t* base, int bytes, uint32_t off, u32x4* r) {
     const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
 #pragma unroll
-    for (int u = 0; u < NI; ++u) r[u] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, off, u * 1024, 2));
+    for (int u = 0; u < NI; ++u) r[u] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, off, u * 1024, NT ? 2 : 0));
 }
 
-template <int D, int RT, int W, int LENS>
+template <int D, int RT, int W, int LENS, bool GROUPED = false>
 __global__ __launch_bounds__(64 * W, RT == 1 ? 3 : 2) void kv8_decode_kernel(const Kv8Decode P) {
     const DecodeParams& p = P.d;
     constexpr int S = D / 64, DT = D / 16, NI = D / 16, BYTES = BN * D;
@@ -57,20 +62,25 @@ __global__ __launch_bounds__(64 * W, RT == 1 ? 3 : 2) void kv8_decode_kernel(con
     __shared__ __attribute__((aligned(16))) float ex[W * WS];
     const int lane = threadIdx.x & 63, ql = lane & 15, kg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int rows = p.g, hkv = LENS == LENS_FIXED ? blockIdx.y : blockIdx.z;
-    int b = LENS == LENS_FIXED ? blockIdx.z : blockIdx.y, r = blockIdx.x, nb = p.n_splits;
+    const int hkv = LENS == LENS_FIXED ? blockIdx.y : blockIdx.z;
+    int b = LENS == LENS_FIXED ? blockIdx.z : blockIdx.y, r = GROUPED ? blockIdx.x / P.groups : blockIdx.x, nb = p.n_splits;
+    const int tok0 = GROUPED ? (blockIdx.x - r * P.groups) * P.tokens : 0;  // the first of its tokens
+    const int ntok = GROUPED ? min(P.tokens, P.n_q - tok0) : P.n_q, rows = GROUPED ? P.g * ntok : p.g;
+    // of a column's row among the entry's
+    auto row_of = [&](int col) { return GROUPED ? (hkv * P.g + col / ntok) * P.n_q + tok0 + col % ntok : hkv * rows + col; };
     const int w = b * p.n_splits + r;  // range of the batch's list
     if (LENS == LENS_DEALT) {
         const Ranges rg = varlen_find(p, lane, w, 0);
         if (rg.b < 0) return;  // (the same in all waves of the workgroup)
         b = rg.b; r = w - rg.first; nb = rg.nb;
-        if (r == 0 && hkv == 0 && threadIdx.x == 0) {  // (every entry has a range)
+        if (r == 0 && hkv == 0 && tok0 == 0 && threadIdx.x == 0) {  // (every entry has a range)
             p.dealt[2 * b] = rg.first;
             p.dealt[2 * b + 1] = nb;
         }
     }
-    const size_t slot = (size_t)w * p.Hq + hkv * rows;
-    const int len = LENS == LENS_ONE ? p.n_keys : __builtin_amdgcn_readfirstlane(min(max(p.seq_lens[b], 0), p.n_cap));
+    const size_t slot = (size_t)w * p.Hq;
+    const int all = LENS == LENS_ONE ? p.n_keys : __builtin_amdgcn_readfirstlane(min(max(p.seq_lens[b], 0), p.n_cap));
+    const int len = GROUPED ? max(all - P.n_q + tok0 + ntok, 0) : all;  // keys that the last of its tokens sees
     const int Tc = (len + BN - 1) / BN, per = (Tc + nb - 1) / nb;
     const int r0 = r * per, r1 = min(Tc, r0 + per);
     const size_t bh = (size_t)b * p.Hkv + hkv;
@@ -84,12 +94,12 @@ __global__ __launch_bounds__(64 * W, RT == 1 ? 3 : 2) void kv8_decode_kernel(con
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         const int row = min(16 * rt + ql, rows - 1);
-        const uint16_t* const q = p.Q + ((size_t)b * p.Hq + hkv * rows + row) * D;
+        const uint16_t* const q = p.Q + ((size_t)b * p.Hq + row_of(row)) * D;
 #pragma unroll
         for (int s = 0; s < 2 * S; ++s) qf[rt][s] = *reinterpret_cast<const bf16x8*>(q + 64 * (s >> 1) + 16 * kg + 8 * (s & 1));
-        sees[rt] = len - P.n_q + 1 + row % P.n_q;
+        sees[rt] = len - ntok + 1 + row % ntok;
     }
-    const int all_see = len - P.n_q + 1;  // keys below are seen by every row
+    const int all_see = len - ntok + 1;  // keys below are seen by every row
     f32x4 ot[RT][DT];
     float m2[RT], lsum[RT];
 #pragma unroll
@@ -104,11 +114,11 @@ __global__ __launch_bounds__(64 * W, RT == 1 ? 3 : 2) void kv8_decode_kernel(con
     auto want = [&](int t) { return t < r1 ? BYTES : 0; };
     auto request_k = [&](int t) __attribute__((always_inline)) {
         sk = KS[min(t, r1 - 1)];
-        kv8_request<NI>(K8 + (size_t)t * BYTES, want(t), off, rk);
+        kv8_request<NI, !GROUPED>(K8 + (size_t)t * BYTES, want(t), off, rk);
     };
     auto request_v = [&](int t) __attribute__((always_inline)) {
         sv = VS[min(t, r1 - 1)];
-        kv8_request<NI>(V8 + (size_t)t * BYTES, want(t), off, rv);
+        kv8_request<NI, !GROUPED>(V8 + (size_t)t * BYTES, want(t), off, rv);
     };
     // tile t; EDGE: some row does not see all of it (there are two such tiles at most, so a wave has one at most, as its last)
     static_assert(W >= 2, "the two tiles that some rows see in part are the last of two waves");
@@ -272,15 +282,16 @@ __global__ __launch_bounds__(64 * W, RT == 1 ? 3 : 2) void kv8_decode_kernel(con
             o += a * *reinterpret_cast<const f32x4*>(ex + v * WS + col * OROW + 4 * c4);
         }
         if (p.n_splits == 1) {  // the only range: this is the result
-            const size_t row = (size_t)b * p.Hq + hkv * rows + col;
+            const size_t row = (size_t)b * p.Hq + row_of(col);
             const float inv = lt == 0.f ? 0.f : 1.f / lt;
             *reinterpret_cast<u32x2*>(p.O + row * D + 4 * c4) = u32x2{pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
             if (p.LSE && c4 == 0) p.LSE[row] = lt == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(lt)) * kLn2;
         } else {
-            *reinterpret_cast<f32x4*>(p.opart + (slot + col) * D + 4 * c4) = o;
+            const size_t row = slot + row_of(col);
+            *reinterpret_cast<f32x4*>(p.opart + row * D + 4 * c4) = o;
             if (c4 == 0) {
-                p.pm[slot + col] = m;
-                p.lpart[slot + col] = lt;
+                p.pm[row] = m;
+                p.lpart[row] = lt;
             }
         }
     }

@@ -167,6 +167,10 @@ int vfa_kv8_decode_splits(int B, int Hq, int Hkv, int n_q, int d, int n_keys, in
     const int n_cu = cu_count() > 0 ? cu_count() : 256, all = ceil_div(n_keys, BN);
     const long long heads = (long long)B * Hkv, rows = (long long)(Hq / Hkv) * n_q;
     if (all <= (d == 64 ? 16 : 12)) return 1;
+    if (rows > 32) {  // two workgroups for each compute unit (32 heads over 8, 64 of 16384 tokens: 1 range 81 us, 2 48, 4 44, 8 46; 256: 1 91, 2 93, 4 101)
+        const int g = Hq / Hkv, tokens = g < 32 ? 32 / g : 1;
+        return (int)max(1LL, min(2LL * n_cu / (heads * ceil_div(n_q, tokens)), (all + 3) / 4LL));
+    }
     const bool dealt = varlen && B > 1 && rows <= 16;
     const long long n = (dealt ? 3LL * n_cu + (d == 64 ? heads - 1 : 0) : (long long)n_cu) / heads;
     return (int)max(1LL, min(n, (all + 3) / 4LL));
@@ -186,18 +190,22 @@ int vfa_kv8_decode_fwd(const void* Q, const void* K8, const void* V8, const void
     if (rc != VFA_OK) return rc;
     if (Hq <= 0 || Hq % Hkv != 0 || n_q < 0 || n_splits < 1 || n_splits > 4096 || !isfinite(softmax_scale)) return VFA_ERR_INVALID_ARG;
     if (!aligned4(seq_lens) || (!seq_lens && (n_keys < 0 || n_keys > n_cap))) return VFA_ERR_INVALID_ARG;
-    const long long rows = (long long)(Hq / Hkv) * n_q;
-    if (rows > 32) return VFA_ERR_UNSUPPORTED;
+    const int g = Hq / Hkv;
+    if (g > 32) return VFA_ERR_UNSUPPORTED;
+    const long long rows = (long long)g * n_q;
     if (done || n_q == 0) return VFA_OK;
     if (!Q || !O || !aligned16(Q) || !aligned16(O) || !aligned4(LSE)) return VFA_ERR_INVALID_ARG;
-    if ((long long)B * Hq * n_q > 0x7fffffffLL) return VFA_ERR_UNSUPPORTED;
+    const bool grouped = rows > 32;
+    const int tokens = grouped ? 32 / g : n_q, groups = ceil_div(n_q, tokens);
+    const long long out_rows = (long long)B * Hq * n_q, wgs = (long long)B * Hkv * n_splits * groups;
+    if (out_rows > 0x7fffffffLL || wgs > kMaxWorkgroups256 || (n_splits > 1 && out_rows > kMaxWorkgroups256)) return VFA_ERR_UNSUPPORTED;
     if (n_splits > 1 && (!workspace || !aligned16(workspace) || workspace_bytes < vfa_kv8_decode_workspace_bytes(B, Hq, n_q, d, n_splits)))
         return VFA_ERR_INVALID_ARG;
     if (n_cap == 0) n_splits = 1;  // (no keys, so no ranges to deal out)
     Kv8Decode P{};
     DecodeParams& p = P.d;
     P.K8 = (const uint8_t*)K8; P.V8 = (const uint8_t*)V8; P.KS = (const uint8_t*)KS; P.VS = (const uint8_t*)VS;
-    P.T = n_cap / BN; P.n_q = n_q;
+    P.T = n_cap / BN; P.n_q = n_q; P.g = g; P.tokens = tokens; P.groups = groups;
     p.Q = (const uint16_t*)Q; p.O = (uint16_t*)O; p.LSE = LSE;
     p.B = B; p.Hq = Hq * n_q; p.Hkv = Hkv; p.n_cap = n_cap; p.n_keys = seq_lens ? n_cap : n_keys; p.seq_lens = seq_lens; p.n_splits = n_splits;
     p.g = (int)rows;
@@ -207,15 +215,13 @@ int vfa_kv8_decode_fwd(const void* Q, const void* K8, const void* V8, const void
     hipStream_t s = (hipStream_t)stream;
     const int n_cu = cu_count() > 0 ? cu_count() : 256;
     (void)hipGetLastError();
-    const long long wgs = (long long)B * Hkv * n_splits;
-    if (wgs > kMaxWorkgroups256) return VFA_ERR_UNSUPPORTED;
-    const bool dealt = seq_lens && n_splits > 1 && B > 1 && (B <= 64 || (B <= DEAL_MAX_B && wgs <= 8LL * n_cu && ceil_div(n_cap, BN) > 2 * n_splits));
+    const bool dealt = seq_lens && n_splits > 1 && B > 1 && (B <= 64 || (B <= DEAL_MAX_B && (long long)B * Hkv * n_splits <= 8LL * n_cu && ceil_div(n_cap, BN) > 2 * n_splits));
     with_d(d, [&](auto d_c) {
         constexpr int D = decltype(d_c)::value;
         // Waves of a workgroup: four have 64 KiB on their way at d = 128, which is what a compute unit gets at a time (one workgroup of 8 waves
         // takes as long for 2048 keys as one of 4, 13 us); d = 64 has half as much in a wave, and one long range eight waves (32 heads of 2048 keys
         // 9.9 / 8.2 us, 128 of 32768 119 / 94)
-        const bool wide = D == 64 && n_splits == 1 && p.n_keys > 1024;
+        const bool wide = D == 64 && n_splits == 1 && p.n_keys > 1024 && !grouped;
         auto launch = [&](auto rt_c, auto w_c) {
             constexpr int RT = decltype(rt_c)::value, W = decltype(w_c)::value;
             const dim3 grid((unsigned)n_splits, (unsigned)B, (unsigned)Hkv);
@@ -229,7 +235,14 @@ int vfa_kv8_decode_fwd(const void* Q, const void* K8, const void* V8, const void
             else kv8_decode_kernel<D, RT, W, LENS_FIXED><<<dim3((unsigned)n_splits, (unsigned)Hkv, (unsigned)B), 64 * W, 0, s>>>(P);
         };
         using std::integral_constant;
+        if (grouped) {
+            const unsigned x = (unsigned)(groups * n_splits);
+            if (!seq_lens) kv8_decode_kernel<D, 2, 4, LENS_ONE, true><<<dim3(x, (unsigned)B, (unsigned)Hkv), 256, 0, s>>>(P);
+            else if (dealt) kv8_decode_kernel<D, 2, 4, LENS_DEALT, true><<<dim3(x, (unsigned)B, (unsigned)Hkv), 256, 0, s>>>(P);
+            else kv8_decode_kernel<D, 2, 4, LENS_FIXED, true><<<dim3(x, (unsigned)Hkv, (unsigned)B), 256, 0, s>>>(P);
+        }
         auto sized = [&](auto w_c) {
+            if (grouped) return;
             if (rows <= 16) launch(integral_constant<int, 1>{}, w_c);
             else launch(integral_constant<int, 2>{}, w_c);
         };
