@@ -18,9 +18,9 @@ namespace {
 // codes are cleared: 0 * NaN).  A NaN in the value of a key that only some of the tokens see would reach the others through weights of zero: it is
 // cleared, too, and the sums of those who see it are set.
 // More than 32 rows (GROUPED: a prompt in pieces) are cut into groups of as many tokens as give 32, each with a workgroup of its own for each range; its last
-// token's keys take the place of the sequence's.  The groups of a KV head, next to each other in the grid, find its tiles in L2, so their loads are not
-// non-temporal, and the matrix unit is what bounds them: the last 1024 of 16384 tokens of 32 heads over 8, D = 128, 308 us (864 TFLOP/s), all of 2 x 16384
-// 4.51 ms (976), 64 of 16384 46 us.  (The scores cost as many conversions for 32 rows as for one.)
+// token's keys take the place of the sequence's.  The KV heads come first in the grid, so that eights of them have an XCD each, in whose L2 their groups find the
+// tiles (groups first: 64 of 16384 tokens of 32 heads over 8 47 us, 32 now; 8 x 64 of 4096 81, 45), and the loads are not non-temporal.  The matrix unit is what
+// bounds them: D = 128, the last 1024 of 16384 tokens 300 us (887 TFLOP/s), all of 2 x 16384 4.55 ms (967).
 // Partial sums of ranges and their merge: decode.hpp, a row for a head.
 struct Kv8Decode {
     DecodeParams d;  // Hq, g: rows for heads (query heads times new tokens); K, V not used
@@ -62,9 +62,9 @@ __global__ __launch_bounds__(64 * W, RT == 1 ? 3 : 2) void kv8_decode_kernel(con
     __shared__ __attribute__((aligned(16))) float ex[W * WS];
     const int lane = threadIdx.x & 63, ql = lane & 15, kg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int hkv = LENS == LENS_FIXED ? blockIdx.y : blockIdx.z;
-    int b = LENS == LENS_FIXED ? blockIdx.z : blockIdx.y, r = GROUPED ? blockIdx.x / P.groups : blockIdx.x, nb = p.n_splits;
-    const int tok0 = GROUPED ? (blockIdx.x - r * P.groups) * P.tokens : 0;  // the first of its tokens
+    const int hkv = GROUPED ? blockIdx.x : LENS == LENS_FIXED ? blockIdx.y : blockIdx.z;
+    int b = GROUPED || LENS == LENS_FIXED ? blockIdx.z : blockIdx.y, r = GROUPED ? blockIdx.y / P.groups : blockIdx.x, nb = p.n_splits;
+    const int tok0 = GROUPED ? (blockIdx.y - r * P.groups) * P.tokens : 0;  // the first of its tokens
     const int ntok = GROUPED ? min(P.tokens, P.n_q - tok0) : P.n_q, rows = GROUPED ? P.g * ntok : p.g;
     // of a column's row among the entry's
     auto row_of = [&](int col) { return GROUPED ? (hkv * P.g + col / ntok) * P.n_q + tok0 + col % ntok : hkv * rows + col; };

@@ -167,7 +167,7 @@ int vfa_kv8_decode_splits(int B, int Hq, int Hkv, int n_q, int d, int n_keys, in
     const int n_cu = cu_count() > 0 ? cu_count() : 256, all = ceil_div(n_keys, BN);
     const long long heads = (long long)B * Hkv, rows = (long long)(Hq / Hkv) * n_q;
     if (all <= (d == 64 ? 16 : 12)) return 1;
-    if (rows > 32) {  // two workgroups for each compute unit (32 heads over 8, 64 of 16384 tokens: 1 range 81 us, 2 48, 4 44, 8 46; 256: 1 91, 2 93, 4 101)
+    if (rows > 32) {  // two workgroups for each compute unit (32 heads over 8, 64 of 16384 tokens: 1 range 80 us, 2 48, 4 32, 8 32; 256: 1 90, 2 93, 4 101)
         const int g = Hq / Hkv, tokens = g < 32 ? 32 / g : 1;
         return (int)max(1LL, min(2LL * n_cu / (heads * ceil_div(n_q, tokens)), (all + 3) / 4LL));
     }
@@ -198,6 +198,7 @@ int vfa_kv8_decode_fwd(const void* Q, const void* K8, const void* V8, const void
     const bool grouped = rows > 32;
     const int tokens = grouped ? 32 / g : n_q, groups = ceil_div(n_q, tokens);
     const long long out_rows = (long long)B * Hq * n_q, wgs = (long long)B * Hkv * n_splits * groups;
+    if (grouped && (long long)groups * n_splits > 65535) return VFA_ERR_UNSUPPORTED;
     if (out_rows > 0x7fffffffLL || wgs > kMaxWorkgroups256 || (n_splits > 1 && out_rows > kMaxWorkgroups256)) return VFA_ERR_UNSUPPORTED;
     if (n_splits > 1 && (!workspace || !aligned16(workspace) || workspace_bytes < vfa_kv8_decode_workspace_bytes(B, Hq, n_q, d, n_splits)))
         return VFA_ERR_INVALID_ARG;
@@ -236,10 +237,10 @@ int vfa_kv8_decode_fwd(const void* Q, const void* K8, const void* V8, const void
         };
         using std::integral_constant;
         if (grouped) {
-            const unsigned x = (unsigned)(groups * n_splits);
-            if (!seq_lens) kv8_decode_kernel<D, 2, 4, LENS_ONE, true><<<dim3(x, (unsigned)B, (unsigned)Hkv), 256, 0, s>>>(P);
-            else if (dealt) kv8_decode_kernel<D, 2, 4, LENS_DEALT, true><<<dim3(x, (unsigned)B, (unsigned)Hkv), 256, 0, s>>>(P);
-            else kv8_decode_kernel<D, 2, 4, LENS_FIXED, true><<<dim3(x, (unsigned)Hkv, (unsigned)B), 256, 0, s>>>(P);
+            const dim3 grid((unsigned)Hkv, (unsigned)(groups * n_splits), (unsigned)B);
+            if (!seq_lens) kv8_decode_kernel<D, 2, 4, LENS_ONE, true><<<grid, 256, 0, s>>>(P);
+            else if (dealt) kv8_decode_kernel<D, 2, 4, LENS_DEALT, true><<<grid, 256, 0, s>>>(P);
+            else kv8_decode_kernel<D, 2, 4, LENS_FIXED, true><<<grid, 256, 0, s>>>(P);
         }
         auto sized = [&](auto w_c) {
             if (grouped) return;
