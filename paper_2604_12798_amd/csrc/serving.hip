@@ -74,9 +74,10 @@ int vfa_qk_norm_rope_fwd(const void* Xq, const void* Xk, const void* Xv, void* Q
     // below 3 x 777 of 24, d = 64, 14 MiB, 5.7 / 6.2), if each covers whole lines of 128 bytes; in parts, a line is fetched twice (7 x 2495 of 96, d = 64, 101 / 128;
     // 2 x 6240 of 80, half of the features rotated, 112 / 131)
     const int n_cu = cu_count() > 0 ? cu_count() : 256;
-    const bool few = wgs * ((heads + 3) / 4) < 2 * n_cu, stream_past = tokens * heads * d >= 1LL << 26 && d == 128 && (interleaved || rot_dim % 128 == 0);
+    const bool few = wgs * ((heads + 3) / 4) < 2 * n_cu;
     const long long ys = few ? heads : (heads + 3) / 4;
     if (ys > 65535 || wgs * ys > kMaxWorkgroups256) return VFA_ERR_UNSUPPORTED;
+    const bool stream_past = tokens * heads * d >= 1LL << 26 && d == 128 && (interleaved || rot_dim % 128 == 0);
     const dim3 grid((unsigned)wgs, (unsigned)ys);
     hipStream_t s = (hipStream_t)stream;
     (void)hipGetLastError();
@@ -160,8 +161,8 @@ int vfa_kv8_read(const void* K8, const void* V8, const void* KS, const void* VS,
 // partial sums (32 heads of 32768 keys, d = 128: 8 ranges 45.0, 12 46.8, 16 49.5, 24 45.7; 128 of 4224: 1 27.0, 2 26.0, 3 27.0, 6 25.8; d = 64, 128 of
 // 32768: 1 119, 2 80, 3 85, 6 83).  Where lengths differ and ranges are dealt out, as many as the units hold at a time, three each, so that what a range is
 // longer than the mean weighs less (128 heads of 200 to 8192 keys: 2 ranges 30.2, 4 29.0, 6 27.8, 8 29.9; 512 of 200 to 2048: 1 29.1, 2 33.2; more fit
-// in at d = 64, 288 heads of 300 to 6175 keys: 2 30.2, 3 26.9, 4 26.8); but
-// one where more than 16 rows make more of the merge: 32 heads of 32 rows of 500 to 8192 keys: 4 ranges 16.9, 8 16.3, 16 19.4, 24 22.9).
+// in at d = 64, 288 heads of 300 to 6175 keys: 2 30.2, 3 26.9, 4 26.8); but one where
+// more than 16 rows make more of the merge (32 heads of 32 rows of 500 to 8192 keys: 4 ranges 16.9, 8 16.3, 16 19.4, 24 22.9).
 int vfa_kv8_decode_splits(int B, int Hq, int Hkv, int n_q, int d, int n_keys, int varlen) {
     if (B <= 0 || Hq <= 0 || Hkv <= 0 || n_q <= 0 || n_keys <= 0) return 1;
     const int n_cu = cu_count() > 0 ? cu_count() : 256, all = ceil_div(n_keys, BN);
@@ -169,7 +170,7 @@ int vfa_kv8_decode_splits(int B, int Hq, int Hkv, int n_q, int d, int n_keys, in
     if (all <= (d == 64 ? 16 : 12)) return 1;
     if (rows > 32) {  // two workgroups for each compute unit (32 heads over 8, 64 of 16384 tokens: 1 range 80 us, 2 48, 4 32, 8 32; 256: 1 90, 2 93, 4 101)
         const int g = Hq / Hkv, tokens = g < 32 ? 32 / g : 1;
-        return (int)max(1LL, min(2LL * n_cu / (heads * ceil_div(n_q, tokens)), (all + 3) / 4LL));
+        return (int)max(1LL, min(2LL * n_cu / (heads * (((long long)n_q + tokens - 1) / tokens)), (all + 3) / 4LL));
     }
     const bool dealt = varlen && B > 1 && rows <= 16;
     const long long n = (dealt ? 3LL * n_cu + (d == 64 ? heads - 1 : 0) : (long long)n_cu) / heads;
@@ -196,9 +197,10 @@ int vfa_kv8_decode_fwd(const void* Q, const void* K8, const void* V8, const void
     if (done || n_q == 0) return VFA_OK;
     if (!Q || !O || !aligned16(Q) || !aligned16(O) || !aligned4(LSE)) return VFA_ERR_INVALID_ARG;
     const bool grouped = rows > 32;
-    const int tokens = grouped ? 32 / g : n_q, groups = ceil_div(n_q, tokens);
-    const long long out_rows = (long long)B * Hq * n_q, wgs = (long long)B * Hkv * n_splits * groups;
-    if (grouped && (long long)groups * n_splits > 65535) return VFA_ERR_UNSUPPORTED;
+    const int tokens = grouped ? 32 / g : n_q;
+    const long long groups = ((long long)n_q + tokens - 1) / tokens, out_rows = (long long)B * Hq * n_q;
+    if (grouped && groups * n_splits > 65535) return VFA_ERR_UNSUPPORTED;
+    const long long wgs = (long long)B * Hkv * n_splits * groups;
     if (out_rows > 0x7fffffffLL || wgs > kMaxWorkgroups256 || (n_splits > 1 && out_rows > kMaxWorkgroups256)) return VFA_ERR_UNSUPPORTED;
     if (n_splits > 1 && (!workspace || !aligned16(workspace) || workspace_bytes < vfa_kv8_decode_workspace_bytes(B, Hq, n_q, d, n_splits)))
         return VFA_ERR_INVALID_ARG;
@@ -206,7 +208,7 @@ int vfa_kv8_decode_fwd(const void* Q, const void* K8, const void* V8, const void
     Kv8Decode P{};
     DecodeParams& p = P.d;
     P.K8 = (const uint8_t*)K8; P.V8 = (const uint8_t*)V8; P.KS = (const uint8_t*)KS; P.VS = (const uint8_t*)VS;
-    P.T = n_cap / BN; P.n_q = n_q; P.g = g; P.tokens = tokens; P.groups = groups;
+    P.T = n_cap / BN; P.n_q = n_q; P.g = g; P.tokens = tokens; P.groups = (int)groups;
     p.Q = (const uint16_t*)Q; p.O = (uint16_t*)O; p.LSE = LSE;
     p.B = B; p.Hq = Hq * n_q; p.Hkv = Hkv; p.n_cap = n_cap; p.n_keys = seq_lens ? n_cap : n_keys; p.seq_lens = seq_lens; p.n_splits = n_splits;
     p.g = (int)rows;
@@ -236,21 +238,20 @@ int vfa_kv8_decode_fwd(const void* Q, const void* K8, const void* V8, const void
             else kv8_decode_kernel<D, RT, W, LENS_FIXED><<<dim3((unsigned)n_splits, (unsigned)Hkv, (unsigned)B), 64 * W, 0, s>>>(P);
         };
         using std::integral_constant;
+        auto sized = [&](auto w_c) {
+            if (rows <= 16) launch(integral_constant<int, 1>{}, w_c);
+            else launch(integral_constant<int, 2>{}, w_c);
+        };
         if (grouped) {
             const dim3 grid((unsigned)Hkv, (unsigned)(groups * n_splits), (unsigned)B);
             if (!seq_lens) kv8_decode_kernel<D, 2, 4, LENS_ONE, true><<<grid, 256, 0, s>>>(P);
             else if (dealt) kv8_decode_kernel<D, 2, 4, LENS_DEALT, true><<<grid, 256, 0, s>>>(P);
             else kv8_decode_kernel<D, 2, 4, LENS_FIXED, true><<<grid, 256, 0, s>>>(P);
+        } else if (wide) {
+            if constexpr (D == 64) sized(integral_constant<int, 8>{});
+        } else {
+            sized(integral_constant<int, 4>{});
         }
-        auto sized = [&](auto w_c) {
-            if (grouped) return;
-            if (rows <= 16) launch(integral_constant<int, 1>{}, w_c);
-            else launch(integral_constant<int, 2>{}, w_c);
-        };
-        if constexpr (D == 64) {
-            if (wide) sized(integral_constant<int, 8>{});
-        }
-        if (!wide) sized(integral_constant<int, 4>{});
         if (n_splits == 1) return;
         const dim3 grid((unsigned)p.Hq, (unsigned)B);
         if (dealt) decode_merge_kernel<D, SLOTS_TABLE, true><<<grid, 256, 0, s>>>(p);

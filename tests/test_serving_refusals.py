@@ -85,7 +85,7 @@ def test_decode(L):
                 dict(scale=float("nan")), dict(scale=float("inf")), dict(Q=NONE), dict(O=NONE), dict(Q=ODD), dict(O=ODD), dict(LSE=ODD), dict(K8=NONE), dict(KS=NONE),
                 dict(V8=ODD), dict(ws=NONE), dict(ws=ODD), dict(bytes=100)):
         assert call(f, good, **bad) == INVALID, bad
-    for bad in (dict(d=32), dict(cap=127), dict(Hq=66), dict(B=40000), dict(Hq=66, n_q=2), dict(n_q=1 << 29), dict(n_q=1 << 24), dict(Hq=32, n_q=65536 * 2 + 1), dict(B=20000, n_q=20000)):
+    for bad in (dict(d=32), dict(cap=127), dict(Hq=66), dict(B=40000), dict(Hq=66, n_q=2), dict(n_q=1 << 29), dict(n_q=1 << 24), dict(Hq=32, n_q=65536 * 2 + 1), dict(B=20000, n_q=20000), dict(Hq=1, Hkv=1, n_q=2 ** 31 - 1)):
         assert call(f, good, **bad) == UNSUPPORTED, bad
     assert L.vfa_kv8_decode_workspace_bytes(2, 8, 3, 64, 5) == (2 * 8 * 3 * 5 * 66 * 4 + 16 + 255) // 256 * 256
     assert L.vfa_kv8_decode_workspace_bytes(0, 8, 3, 64, 5) == 0 and L.vfa_kv8_decode_workspace_bytes(1, 8, 0, 64, 5) == 0
@@ -93,6 +93,7 @@ def test_decode(L):
         for d in (64, 128):
             for varlen in (0, 1):
                 assert 1 <= L.vfa_kv8_decode_splits(B, 4 * H, H, 2, d, n, varlen) <= 4096
+    assert L.vfa_kv8_decode_splits(1, 64, 1, 2 ** 31 - 1, 64, 2 ** 31 - 64, 1) == 1 and L.vfa_kv8_decode_splits(1, 1, 1, 2 ** 31 - 1, 64, 4096, 0) == 1
     assert L.vfa_kv8_decode_splits(1, 0, 1, 1, 64, 4096, 0) == 1 and L.vfa_kv8_decode_splits(1, 1, 1, 0, 64, 4096, 0) == 1
 
 
