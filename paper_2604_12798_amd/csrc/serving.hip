@@ -155,25 +155,30 @@ int vfa_kv8_read(const void* K8, const void* V8, const void* KS, const void* VS,
     return launched();
 }
 
-// One range for each KV head, which is one launch and no partial sums, where there are few keys (us, one range / the best number of ranges: 8 heads of
-// 768 keys, d = 128, 6.1 / 6.8, of 1024 7.0 / 6.5, of 1536 10.2 / 7.2; 16 of 1024, d = 64, 5.2 / 6.5, of 2048 9.9 / 6.7; 128 of 1024 9.3 / 11.2).
+// One range for each KV head, which is one launch and no partial sums, where there are few keys, and more of them the more units the heads fill (us, one range /
+// the best number of ranges; d = 128: 8 heads of 768 keys 6.1 / 6.8, of 1024 7.0 / 6.5, of 1536 10.2 / 7.2; 128 of 1536 12.2 / 12.8, of 200 to 2048 14.1 / 13.1;
+// 256 of 100 to 1024 10.2 / 13.5, of 200 to 2048 16.6 / 18.7, of 200 to 4096 29.9 / 29.9; d = 64: 16 of 1024 5.2 / 6.5, of 2048 9.9 / 6.7; 128 of 100 to 2048
+// 8.6 / 10.0; 256 of as many 10.0 / 12.8, 288 of 300 to 6175 25.5 / 26.8).
 // Else as many workgroups as there are compute units where all are equally long: a unit has 64 KiB on their way to it in either case, and fewer
 // partial sums (32 heads of 32768 keys, d = 128: 8 ranges 45.0, 12 46.8, 16 49.5, 24 45.7; 128 of 4224: 1 27.0, 2 26.0, 3 27.0, 6 25.8; d = 64, 128 of
 // 32768: 1 119, 2 80, 3 85, 6 83).  Where lengths differ and ranges are dealt out, as many as the units hold at a time, three each, so that what a range is
 // longer than the mean weighs less (128 heads of 200 to 8192 keys: 2 ranges 30.2, 4 29.0, 6 27.8, 8 29.9; 512 of 200 to 2048: 1 29.1, 2 33.2; more fit
-// in at d = 64, 288 heads of 300 to 6175 keys: 2 30.2, 3 26.9, 4 26.8); but one where
+// in at d = 64, 288 heads of 300 to 6175 keys: 2 30.2, 3 26.9, 4 26.8), but one where
 // more than 16 rows make more of the merge (32 heads of 32 rows of 500 to 8192 keys: 4 ranges 16.9, 8 16.3, 16 19.4, 24 22.9).
 int vfa_kv8_decode_splits(int B, int Hq, int Hkv, int n_q, int d, int n_keys, int varlen) {
-    if (B <= 0 || Hq <= 0 || Hkv <= 0 || n_q <= 0 || n_keys <= 0) return 1;
+    if (B <= 0 || Hq <= 0 || Hkv <= 0 || n_q <= 0 || n_keys <= 0 || (long long)B * Hkv > 65535) return 1;
     const int n_cu = cu_count() > 0 ? cu_count() : 256, all = ceil_div(n_keys, BN);
-    const long long heads = (long long)B * Hkv, rows = (long long)(Hq / Hkv) * n_q;
-    if (all <= (d == 64 ? 16 : 12)) return 1;
-    if (rows > 32) {  // two workgroups for each compute unit (32 heads over 8, 64 of 16384 tokens: 1 range 80 us, 2 48, 4 32, 8 32; 256: 1 90, 2 93, 4 101)
-        const int g = Hq / Hkv, tokens = g < 32 ? 32 / g : 1;
-        return (int)max(1LL, min(2LL * n_cu / (heads * (((long long)n_q + tokens - 1) / tokens)), (all + 3) / 4LL));
-    }
+    const long long rows = (long long)(Hq / Hkv) * n_q;
+    const int g = Hq / Hkv, tokens = rows <= 32 ? n_q : g < 32 ? 32 / g : 1;
+    const long long heads = (long long)B * Hkv * (((long long)n_q + tokens - 1) / tokens);  // (with more than 32 rows, groups of them)
+    const int most = heads >= n_cu ? (d == 64 ? 96 : 64) : 2 * heads >= n_cu ? (d == 64 ? 40 : 28) : d == 64 ? 16 : 12;
+    if (all <= most) return 1;
+    // more than 32 rows: two workgroups for each compute unit (32 heads over 8, 64 of 16384 tokens: 1 range 80 us, 2 48, 4 32, 8 32; 256: 1 90, 2 93, 4 101)
+    if (rows > 32) return (int)max(1LL, min(2LL * n_cu / heads, (all + 3) / 4LL));
     const bool dealt = varlen && B > 1 && rows <= 16;
-    const long long n = (dealt ? 3LL * n_cu + (d == 64 ? heads - 1 : 0) : (long long)n_cu) / heads;
+    long long n = (dealt ? 3LL * n_cu + (d == 64 ? heads - 1 : 0) : (long long)n_cu) / heads;
+    // no range without a tile for each of its waves, and two if there are enough for the units (64 heads of 2000 keys: 4 ranges 11.2, 8 12.3)
+    if (dealt) n = min(n, max((all + 7) / 8LL, (n_cu + heads - 1) / heads));
     return (int)max(1LL, min(n, (all + 3) / 4LL));
 }
 

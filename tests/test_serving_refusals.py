@@ -94,6 +94,8 @@ def test_decode(L):
             for varlen in (0, 1):
                 assert 1 <= L.vfa_kv8_decode_splits(B, 4 * H, H, 2, d, n, varlen) <= 4096
     assert L.vfa_kv8_decode_splits(1, 64, 1, 2 ** 31 - 1, 64, 2 ** 31 - 64, 1) == 1 and L.vfa_kv8_decode_splits(1, 1, 1, 2 ** 31 - 1, 64, 4096, 0) == 1
+    big = 2 ** 31 - 1
+    assert L.vfa_kv8_decode_splits(big, big, big, big, 64, big, 1) == 1 and L.vfa_kv8_decode_splits(65535, big, 1, big, 128, big, 0) == 1
     assert L.vfa_kv8_decode_splits(1, 0, 1, 1, 64, 4096, 0) == 1 and L.vfa_kv8_decode_splits(1, 1, 1, 0, 64, 4096, 0) == 1
 
 
