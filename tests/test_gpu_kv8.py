@@ -304,6 +304,14 @@ def test_one_length_for_all(vfa, n, n_splits):
     run_decode(vfa, 2, 8, 2, 1024, 64, 3, [n, n], n_splits, uniform=True, seed=n)
 
 
+@pytest.mark.parametrize("d,g,n_q", [(64, 3, 1), (64, 5, 5), (128, 4, 1), (128, 6, 4)])
+@pytest.mark.parametrize("n_splits", [1, 2, 9])
+def test_long_ranges(vfa, d, g, n_q, n_splits):
+    """Ranges of many tiles for each wave, of four waves and of eight (64-wide heads in one range)."""
+    run_decode(vfa, 3, 2 * g, 2, 4096, d, n_q, [4096, 1025, 3001], n_splits, seed=d + g)
+    run_decode(vfa, 2, g, 1, 2048, d, n_q, [2011, 2011], n_splits, seed=d + g, uniform=True)
+
+
 @pytest.mark.parametrize("B,n_splits", [(70, 2), (256, 3), (300, 2), (300, 1), (5000, None)])
 def test_many_sequences(vfa, B, n_splits):
     """Batches whose ranges are dealt out, and batches above that."""
