@@ -74,18 +74,19 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(const RopeParams p) {
         cb = j < pairs8 ? j + pairs8 : j + L;
     }
     float cs[8], sn[8];  // of the pairs in a chunk of each, or of the eight pairs
+    // what is not rotated is not multiplied either: 0 times an infinity beside it would be a NaN
+    const bool turn_a = PAIRS == PAIRS_HALF ? j < pairs8 : ca < 2 * pairs8, turn_b = PAIRS == PAIRS_HALF ? turn_a : cb < 2 * pairs8;
     if (PAIRS != PAIRS_NONE) {
         const int pos = (int)min(max((long long)n + (p.first_pos ? p.first_pos[b] : p.first), 0LL), (long long)p.n_pos - 1);
         const float* const c = p.cos_sin + (size_t)pos * p.rot;
 #pragma unroll
         for (int e4 = 0; e4 < 2; ++e4) {
-            const bool turns = PAIRS == PAIRS_HALF ? j < pairs8 : (e4 ? cb : ca) < 2 * pairs8;
-            const int at = !turns ? 0 : PAIRS == PAIRS_HALF ? 8 * j + 4 * e4 : 4 * (e4 ? cb : ca);
+            const int at = !(e4 ? turn_b : turn_a) ? 0 : PAIRS == PAIRS_HALF ? 8 * j + 4 * e4 : 4 * (e4 ? cb : ca);
             const f32x4 x = *reinterpret_cast<const f32x4*>(c + at), y = *reinterpret_cast<const f32x4*>(c + p.rot / 2 + at);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                cs[4 * e4 + e] = turns ? x[e] : 1.f;
-                sn[4 * e4 + e] = turns ? y[e] : 0.f;
+                cs[4 * e4 + e] = x[e];
+                sn[4 * e4 + e] = y[e];
             }
         }
     }
@@ -126,24 +127,24 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(const RopeParams p) {
                     c[e] *= w ? r * wb[e] : r;
                 }
             }
-            if (PAIRS == PAIRS_HALF) {
+            if (PAIRS == PAIRS_HALF && turn_a) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float za = a[e], zb = c[e];
                     a[e] = za * cs[e] - zb * sn[e];
                     c[e] = zb * cs[e] + za * sn[e];
                 }
-            } else if (PAIRS == PAIRS_NEXT) {
+            }
+            auto next = [&](float* z, const float* co, const float* si) __attribute__((always_inline)) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    float z0 = a[2 * e], z1 = a[2 * e + 1];
-                    a[2 * e] = z0 * cs[e] - z1 * sn[e];
-                    a[2 * e + 1] = z1 * cs[e] + z0 * sn[e];
-                    z0 = c[2 * e]; z1 = c[2 * e + 1];
-                    c[2 * e] = z0 * cs[4 + e] - z1 * sn[4 + e];
-                    c[2 * e + 1] = z1 * cs[4 + e] + z0 * sn[4 + e];
+                    const float z0 = z[2 * e], z1 = z[2 * e + 1];
+                    z[2 * e] = z0 * co[e] - z1 * si[e];
+                    z[2 * e + 1] = z1 * co[e] + z0 * si[e];
                 }
-            }
+            };
+            if (PAIRS == PAIRS_NEXT && turn_a) next(a, cs, sn);
+            if (PAIRS == PAIRS_NEXT && turn_b) next(c, cs + 4, sn + 4);
             ra[u] = pack_bf16x8(a);
             rb[u] = pack_bf16x8(c);
         }

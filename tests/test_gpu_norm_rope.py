@@ -106,3 +106,32 @@ def test_empty(vfa):
     assert Q.shape == (0, 2, 3, 64)
     q = torch.empty((3, 0, 2, 64), dtype=torch.bfloat16, device="cuda")
     assert vfa.qk_norm_rope_fwd(q, q)[1].shape == (3, 2, 0, 64)
+
+
+@pytest.mark.parametrize("d,rot", [(64, 16), (64, 48), (128, 16), (128, 64), (128, 112)])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("norm", [False, True])
+def test_unrotated_features_stand_alone(vfa, d, rot, inter, norm):
+    """An infinity or NaN in each unrotated feature of a token in turn: without the norm no other feature changes, with it an infinity leaves
+    zeros beside it."""
+    kinds = [float("inf"), float("-inf"), float("nan")]
+    N = 3 * (d - rot)
+    clean = rnd((1, N, 3, d), rot, 3.0)
+    x = clean.clone()
+    at = [rot + n // 3 for n in range(N)]
+    for n in range(N):
+        x[0, n, 1, at[n]] = kinds[n % 3]
+    cs = table(N + 2, rot)
+    Q, K, _ = vfa.qk_norm_rope_fwd(x, x, norm=norm, eps=1e-5, cos_sin=cs, interleaved=inter, first_pos=2)
+    assert torch.equal(Q.nan_to_num(7.0), K.nan_to_num(7.0))
+    y, size = ref.norm_rope(x, None, 1e-5, cs, inter, [2], norm)
+    got = Q.double().cpu()
+    assert torch.equal(got.isnan(), y.isnan()) and torch.equal(got.isinf(), y.isinf())
+    fin = y.isfinite()
+    off = (got - y).abs() - 2.0 ** -8 * y.abs() - 2.0 ** -16 * size
+    assert (off[fin] <= 0).all(), off[fin].max().item()
+    if not norm:
+        same = vfa.qk_norm_rope_fwd(clean, clean, norm=False, cos_sin=cs, interleaved=inter, first_pos=2)[0]
+        for n in range(N):
+            same[0, 1, n, at[n]] = x[0, n, 1, at[n]]
+        assert torch.equal(Q.nan_to_num(7.0), same.nan_to_num(7.0))
