@@ -146,6 +146,24 @@ def _stream(stream):
     return _current_stream(_current_device())
 
 
+def _on(stream, f, args):
+    """f(**args) with its `stream` as the current one, for a wrapper that allocates.  Memory for a call on another stream has to be that stream's: in what the
+    current stream gives out, work of its own may still be under way, and a workspace that is dropped at the return would be given out again while the call
+    runs.  Outputs are used on the stream that was current, so they are kept from others until that one is through with them, too."""
+    import torch
+    args["stream"] = None
+    before = torch.cuda.current_stream()
+    if stream == before:
+        return f(**args)
+    with torch.cuda.stream(stream):
+        out = f(**args)
+    given = [x for a in args.values() for x in (a if isinstance(a, (tuple, list)) else (a,))]
+    for t in out if isinstance(out, tuple) else (out,):
+        if t is not None and not any(t is x for x in given):
+            t.record_stream(before)
+    return out
+
+
 def _outputs(Q, out, lse, want_lse):
     if out is None or (lse is None and want_lse):
         import torch
@@ -160,6 +178,8 @@ def _outputs(Q, out, lse, want_lse):
 def kblock_summary(K, block_n: int = 64, out=None, stream=None, repr_mode: int = 0):
     """Key-block summaries Krepr [B, Hkv, ceil(N/block_n), d] (bf16) of K [B, Hkv, N, d].
     repr_mode 0 = sabsmax (the method); 1 / 2 / 3 = per-dimension max / mean / unsigned absmax."""
+    if stream is not None and out is None:
+        return _on(stream, kblock_summary, locals())
     n = _n()
     import torch
     B, Hkv, N, d = K.shape
@@ -176,6 +196,8 @@ def kblock_summary(K, block_n: int = 64, out=None, stream=None, repr_mode: int =
 
 def fa_baseline_fwd(Q, K, V, *, block_m=128, block_n=64, causal=True, softmax_scale=0.0, out=None, lse=None,
                     want_lse=True, stream=None):
+    if stream is not None and (out is None or (lse is None and want_lse)):
+        return _on(stream, fa_baseline_fwd, locals())
     n = _n()
     B, Hq, Hkv, N, d = n.check_qkv(Q, K, V, _bf16)
     O, L = _outputs(Q, out, lse, want_lse)
@@ -188,6 +210,8 @@ def fa_baseline_fwd(Q, K, V, *, block_m=128, block_n=64, causal=True, softmax_sc
 
 def fa_lazy_rescale_fwd(Q, K, V, *, block_m=128, block_n=64, causal=True, softmax_scale=0.0, rescale_tau=8.0, out=None,
                         lse=None, want_lse=True, stream=None):
+    if stream is not None and (out is None or (lse is None and want_lse)):
+        return _on(stream, fa_lazy_rescale_fwd, locals())
     n = _n()
     B, Hq, Hkv, N, d = n.check_qkv(Q, K, V, _bf16)
     O, L = _outputs(Q, out, lse, want_lse)
@@ -200,6 +224,8 @@ def fa_lazy_rescale_fwd(Q, K, V, *, block_m=128, block_n=64, causal=True, softma
 
 def fa_lazy_rescale_softexp_fwd(Q, K, V, *, block_m=128, block_n=64, causal=True, softmax_scale=0.0, rescale_tau=8.0,
                                 out=None, lse=None, want_lse=True, stream=None):
+    if stream is not None and (out is None or (lse is None and want_lse)):
+        return _on(stream, fa_lazy_rescale_softexp_fwd, locals())
     n = _n()
     B, Hq, Hkv, N, d = n.check_qkv(Q, K, V, _bf16)
     O, L = _outputs(Q, out, lse, want_lse)
@@ -221,6 +247,8 @@ def _workspace(Q, K, block_n, workspace):
 
 def vfa_attn_fwd(Q, K, V, *, block_m=128, block_n=64, causal=True, n_sink=1, n_local=1, use_minit=True,
                  softmax_scale=0.0, workspace=None, out=None, lse=None, want_lse=True, stream=None):
+    if stream is not None and (out is None or workspace is None or (lse is None and want_lse)):
+        return _on(stream, vfa_attn_fwd, locals())
     n = _n()
     B, Hq, Hkv, N, d = n.check_qkv(Q, K, V, _bf16)
     O, L = _outputs(Q, out, lse, want_lse)
@@ -236,6 +264,8 @@ def vfa_attn_fwd(Q, K, V, *, block_m=128, block_n=64, causal=True, n_sink=1, n_l
 def vsa_attn_fwd(Q, K, V, *, block_m=128, block_n=64, causal=True, n_sink=1, n_local=1, use_minit=True,
                  softmax_scale=0.0, skip_threshold_nats=8.0, skip_mask=None, want_mask=True, workspace=None,
                  out=None, lse=None, want_lse=True, stream=None):
+    if stream is not None and (out is None or workspace is None or (lse is None and want_lse) or (skip_mask is None and want_mask)):
+        return _on(stream, vsa_attn_fwd, locals())
     n = _n()
     B, Hq, Hkv, N, d = n.check_qkv(Q, K, V, _bf16)
     O, L = _outputs(Q, out, lse, want_lse)
@@ -257,6 +287,8 @@ def vfa_variant_fwd(Q, K, V, *, block_m=128, block_n=64, causal=True, n_sink=1, 
                     skip_threshold_nats=0.0, skip_mask=None,
                     workspace=None, out=None, lse=None, want_lse=True, stream=None):
     """VFA / VSA with the ablation switches; returns (O, LSE, mask) with mask None when nothing is skipped."""
+    if stream is not None and (out is None or workspace is None or (lse is None and want_lse) or (skip_mask is None and skip_threshold_nats != 0.0)):
+        return _on(stream, vfa_variant_fwd, locals())
     import torch
     n = _n()
     B, Hq, Hkv, N, d = n.check_qkv(Q, K, V, _bf16)
@@ -316,6 +348,8 @@ def _decode_outputs(q, n_splits, out, lse, want_lse, workspace):
 def decode_varlen_fwd(q, K, V, seq_lens, *, krepr=None, block_n=64, n_sink=1, n_local=1, use_minit=True, n_splits=8,
                       softmax_scale=0.0, workspace=None, out=None, lse=None, want_lse=True, stream=None):
     """As decode_fwd with per-sequence lengths (int32 device tensor of B entries)."""
+    if stream is not None and (out is None or workspace is None or (lse is None and want_lse)):
+        return _on(stream, decode_varlen_fwd, locals())
     n = _n()
     B, Hq, d, Hkv, n_cap = n.check_cache(q, K, V, None)
     assert seq_lens.is_cuda and seq_lens.dtype == _i32 and seq_lens.numel() == B
@@ -336,6 +370,8 @@ def decode_workspace_bytes(B: int, Hq: int, d: int, n_splits: int) -> int:
 def decode_fwd(q, K, V, n_keys: int, *, krepr=None, block_n=64, n_sink=1, n_local=1, use_minit=True, n_splits=8,
                softmax_scale=0.0, workspace=None, out=None, lse=None, want_lse=True, stream=None):
     """One query token per head, q [B, Hq, d], against the first n_keys rows of the cache K, V [B, Hkv, n_cap, d]."""
+    if stream is not None and (out is None or workspace is None or (lse is None and want_lse)):
+        return _on(stream, decode_fwd, locals())
     n = _n()
     B, Hq, d, Hkv, n_cap = n.check_cache(q, K, V, _bf16)
     O, L, ws = _decode_outputs(q, n_splits, out, lse, want_lse, workspace)
@@ -367,6 +403,8 @@ def decode_noalloc_fwd(q, K, V, n_keys: int, out, lse=None, *, krepr=None, block
 
 def fp8_quantize(X, inv_scale: float, stream=None):
     """bf16 tensor -> uint8 tensor of E4M3 codes of X * inv_scale (same shape)."""
+    if stream is not None:
+        return _on(stream, fp8_quantize, locals())
     n = _n()
     import torch
     assert X.is_cuda and X.dtype == torch.bfloat16 and X.is_contiguous()
@@ -379,6 +417,8 @@ def fp8_quantize(X, inv_scale: float, stream=None):
 
 def fp8_pack_v(V, inv_scale: float, stream=None):
     """V [B, Hkv, N, 128] bf16 -> [B, Hkv, ceil(N/64), 128, 64] uint8 (transposed, key-permuted E4M3 tiles)."""
+    if stream is not None:
+        return _on(stream, fp8_pack_v, locals())
     n = _n()
     import torch
     B, Hkv, N, d = V.shape
@@ -393,6 +433,8 @@ def fp8_attn_fwd(Q8, K8, Vt8, *, descale_q, descale_k, descale_v, frozen=True, b
                  n_sink=1, n_local=1, use_minit=True, softmax_scale=0.0, workspace=None, out=None, lse=None,
                  want_lse=True, stream=None, noexp=False):
     """E4M3 attention; noexp=True calls vfa_fp8_attn_noexp_fwd (Alg. 1 with the weights' codes taken from the scores)."""
+    if stream is not None and (out is None or workspace is None or (lse is None and want_lse)):
+        return _on(stream, fp8_attn_fwd, locals())
     n = _n()
     import torch
     B, Hq, N, d = Q8.shape
@@ -415,6 +457,8 @@ def fp8_attn_fwd(Q8, K8, Vt8, *, descale_q, descale_k, descale_v, frozen=True, b
 
 def mxfp4_quantize(X, pre_scale: float = 1.0, stream=None):
     """bf16 tensor [..., d] (d a multiple of 32) -> (uint8 [..., d/2] E2M1 pairs, uint8 [..., d/32] E8M0 scales) of X * pre_scale."""
+    if stream is not None:
+        return _on(stream, mxfp4_quantize, locals())
     n = _n()
     import torch
     assert X.is_cuda and X.dtype == torch.bfloat16 and X.is_contiguous() and X.shape[-1] % 32 == 0
@@ -436,6 +480,8 @@ def mxfp4_attn_fwd(Q4, QS, K4, KS, Vt8, *, descale_v, frozen=True, block_m=128, 
                    stream=None, noexp=False):
     """Attention with MXFP4 scores (Q4/QS, K4/KS from mxfp4_quantize) and 8-bit P.V (Vt8 from fp8_pack_v);
     noexp=True calls vfa_mxfp4_attn_noexp_fwd."""
+    if stream is not None and (out is None or workspace is None or (lse is None and want_lse)):
+        return _on(stream, mxfp4_attn_fwd, locals())
     n = _n()
     import torch
     B, Hq, N, dh = Q4.shape
@@ -484,6 +530,8 @@ def qk_norm_rope_fwd(q, k, v=None, *, norm=True, q_weight=None, k_weight=None, e
     K, V [B, Hkv, N, d] as the attention calls take them: queries and keys normed over each head (norm=True; weights [d] or None) and
     rotated by position (cos_sin [n_pos, rot] fp32: cosines, then sines; None: no rotation).  first_pos: position of token 0, a
     number or an int32 tensor of B entries.  out: (Q, K, V) to write to."""
+    if stream is not None and out is None:
+        return _on(stream, qk_norm_rope_fwd, locals())
     n = _ns()
     dev, B, N, Hq, Hkv, d, *strides, n_pos, rot, at, first = n.check_norm_rope(q, k, v, q_weight, k_weight, cos_sin, first_pos, _bf16, _f32, _i32)
     _serving(dev)
@@ -528,6 +576,8 @@ def kv8_append(K, V, cache, old_lens, new_lens, stream=None):
 def kv8_read(cache, n: int, *, seq_lens=None, out=None, stream=None):
     """The first n tokens of every sequence in bf16: K, V [B, Hkv, n, d], zeros at and behind seq_lens (a number or an int32 tensor of B
     entries; None: n)."""
+    if stream is not None and out is None:
+        return _on(stream, kv8_read, locals())
     nat = _ns()
     K8, V8, KS, VS = cache
     n = int(n)
@@ -560,6 +610,8 @@ def kv8_decode_fwd(q, cache, seq_lens, *, n_splits=None, softmax_scale=0.0, work
     """Attention of each sequence's newest tokens, q [B, Hq, n_q, d] (or [B, Hq, d] for one), over the cache that holds them already: a step, drafts,
     a piece of a prompt; seq_lens: a number or an int32 tensor of B entries.  n_splits: key ranges (None: vfa_kv8_decode_splits, of the cache's capacity where the
     lengths are on the GPU).  A workspace of kv8_decode_workspace_bytes is for calls that must not allocate."""
+    if stream is not None and (out is None or workspace is None or (lse is None and want_lse)):
+        return _on(stream, kv8_decode_fwd, locals())
     n = _ns()
     K8, V8, KS, VS = cache
     dev, B, Hq, Hkv, n_cap, n_q, d, lens, n_keys = n.check_kv8_decode(q, K8, V8, KS, VS, seq_lens, _bf16, _u8, _i32)
