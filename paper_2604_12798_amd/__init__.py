@@ -514,8 +514,9 @@ def _ns():
     global _empty_like, _f32, _u8, _current_device, _current_stream
     if _empty_like is None:
         import torch
-        _empty_like, _f32, _u8 = torch.empty_like, torch.float32, torch.uint8
+        _f32, _u8 = torch.float32, torch.uint8
         _current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+        _empty_like = torch.empty_like  # (the last one: another thread that finds it here uses all of them)
     return _native or _n()
 
 
