@@ -13,6 +13,7 @@
 
 #include <cstddef>
 #include <cstdint>
+#include <limits>
 #include <tuple>
 #include <type_traits>
 #include <utility>
@@ -68,37 +69,67 @@ bool convert(PyObject* o, T*& v) {
     v = reinterpret_cast<T*>((uintptr_t)PyLong_AsUnsignedLongLongMask(o));
     return true;
 }
+// Whole numbers of the serving operators, whose lengths and positions users count in Python: one that its type does not hold makes the call a refused one
+// (`held`), as the entry point would refuse it if it saw it.
 template <typename T>
-bool convert_tensor(PyObject* o, T& v) {
-    if constexpr (std::is_pointer_v<T>) {
+bool convert_held(PyObject* o, T& v, bool& held) {
+    if constexpr (!std::is_integral_v<T>) {
+        return convert(o, v);
+    } else if constexpr (std::is_signed_v<T>) {
+        int past = 0;
+        const long long x = PyLong_AsLongLongAndOverflow(o, &past);
+        if (x == -1 && !past && PyErr_Occurred()) return false;
+        held = held && !past && x >= std::numeric_limits<T>::min() && x <= std::numeric_limits<T>::max();
+        v = (T)x;
+        return true;
+    } else {
+        static_assert(sizeof(T) == sizeof(unsigned long long));
+        const Ref i(PyNumber_Index(o));
+        if (!i.o) return false;
+        v = (T)PyLong_AsUnsignedLongLong(i.o);
+        if (v != (T)-1 || !PyErr_Occurred()) return true;
+        if (!PyErr_ExceptionMatches(PyExc_OverflowError)) return false;
+        PyErr_Clear();
+        held = false;
+        return true;
+    }
+}
+template <bool TENSORS, bool HELD, typename T>
+bool convert_any(PyObject* o, T& v, bool& held) {
+    if constexpr (TENSORS && std::is_pointer_v<T>) {
         if (o == Py_None) return convert(o, v);
         const Ref p = method(o, names.data_ptr);
         return p.o && convert(p.o, v);
+    } else if constexpr (HELD) {
+        return convert_held(o, v, held);
     } else {
         return convert(o, v);
     }
 }
 
-template <bool TENSORS, typename R, typename... A, size_t... I>
+// REFUSED: nothing, or what the function returns for arguments that it does not take
+template <bool TENSORS, auto... REFUSED, typename R, typename... A, size_t... I>
 PyObject* call(R (*f)(A...), PyObject* const* args, Py_ssize_t n, std::index_sequence<I...>) {
     if (n != (Py_ssize_t)sizeof...(A)) {
         PyErr_Format(PyExc_TypeError, "expected %zd arguments, got %zd", (Py_ssize_t)sizeof...(A), n);
         return nullptr;
     }
     std::tuple<A...> v{};
-    const bool ok = ((TENSORS && I + 1 < sizeof...(A) ? convert_tensor(args[I], std::get<I>(v)) : convert(args[I], std::get<I>(v))) && ...);
+    bool held = true;
+    const bool ok = (convert_any<TENSORS && I + 1 < sizeof...(A), sizeof...(REFUSED) != 0>(args[I], std::get<I>(v), held) && ...);
     if (!ok) return nullptr;
+    if (!held) return PyLong_FromLongLong((0LL + ... + REFUSED));
     R r;
     Py_BEGIN_ALLOW_THREADS  // (as ctypes does: other threads run while the launches are enqueued)
     r = f(std::get<I>(v)...);
     Py_END_ALLOW_THREADS
     return std::is_unsigned_v<R> ? PyLong_FromUnsignedLongLong((unsigned long long)r) : PyLong_FromLongLong((long long)r);
 }
-template <bool TENSORS, auto F>
+template <bool TENSORS, auto F, auto... REFUSED>
 struct Wrap;
-template <bool TENSORS, typename R, typename... A, R (*F)(A...)>
-struct Wrap<TENSORS, F> {
-    static PyObject* run(PyObject*, PyObject* const* args, Py_ssize_t n) { return call<TENSORS>(F, args, n, std::index_sequence_for<A...>{}); }
+template <bool TENSORS, typename R, typename... A, R (*F)(A...), auto... REFUSED>
+struct Wrap<TENSORS, F, REFUSED...> {
+    static PyObject* run(PyObject*, PyObject* const* args, Py_ssize_t n) { return call<TENSORS, REFUSED...>(F, args, n, std::index_sequence_for<A...>{}); }
 };
 
 // is_cuda, dtype, is_contiguous() and, unless dims < 0, dim() of a tensor are as they have to be: 1, 0, or -1 with an error set
@@ -353,6 +384,8 @@ PyObject* check_tensor(PyObject*, PyObject* const* args, Py_ssize_t n) {
 #define VFA_FUNCTION(f) (PyCFunction)(void (*)(void)) & f, METH_FASTCALL, nullptr
 #define VFA_METHOD(name) {#name, VFA_FUNCTION((Wrap<false, &name>::run))}
 #define VFA_METHODS(name) VFA_METHOD(name), {#name "_t", VFA_FUNCTION((Wrap<true, &name>::run))}
+#define VFA_HELD_METHOD(name, refused) {#name, VFA_FUNCTION((Wrap<false, &name, refused>::run))}
+#define VFA_HELD_METHODS(name) VFA_HELD_METHOD(name, VFA_ERR_INVALID_ARG), {#name "_t", VFA_FUNCTION((Wrap<true, &name, VFA_ERR_INVALID_ARG>::run))}
 PyMethodDef methods[] = {
     VFA_METHOD(vfa_workspace_bytes), VFA_METHODS(vfa_kblock_summary), VFA_METHODS(vfa_kblock_summary_mode),
     VFA_METHODS(fa_baseline_fwd), VFA_METHODS(fa_lazy_rescale_fwd), VFA_METHODS(fa_lazy_rescale_softexp_fwd),
@@ -361,8 +394,8 @@ PyMethodDef methods[] = {
     VFA_METHOD(vfa_decode_workspace_bytes), VFA_METHODS(vfa_decode_fwd), VFA_METHODS(vfa_decode_noalloc_fwd), VFA_METHODS(vfa_decode_varlen_fwd),
     VFA_METHODS(vfa_fp8_quantize), VFA_METHOD(vfa_fp8_v_bytes), VFA_METHODS(vfa_fp8_pack_v), VFA_METHODS(vfa_fp8_attn_fwd), VFA_METHODS(vfa_fp8_attn_noexp_fwd),
     VFA_METHODS(vfa_mxfp4_quantize), VFA_METHOD(vfa_mxfp4_workspace_bytes), VFA_METHODS(vfa_mxfp4_attn_fwd), VFA_METHODS(vfa_mxfp4_attn_noexp_fwd),
-    VFA_METHODS(vfa_qk_norm_rope_fwd), VFA_METHODS(vfa_kv8_append), VFA_METHODS(vfa_kv8_read), VFA_METHOD(vfa_kv8_decode_splits),
-    VFA_METHOD(vfa_kv8_decode_workspace_bytes), VFA_METHODS(vfa_kv8_decode_fwd),
+    VFA_HELD_METHODS(vfa_qk_norm_rope_fwd), VFA_HELD_METHODS(vfa_kv8_append), VFA_HELD_METHODS(vfa_kv8_read), VFA_HELD_METHOD(vfa_kv8_decode_splits, 1),
+    VFA_HELD_METHOD(vfa_kv8_decode_workspace_bytes, 0), VFA_HELD_METHODS(vfa_kv8_decode_fwd),
     {"check_qkv", VFA_FUNCTION(check_qkv)}, {"check_cache", VFA_FUNCTION(check_cache)},
     {"check_cache8", VFA_FUNCTION(check_cache8)}, {"check_kv8_append", VFA_FUNCTION(check_kv8_append)},
     {"check_kv8_decode", VFA_FUNCTION(check_kv8_decode)}, {"check_norm_rope", VFA_FUNCTION(check_norm_rope)}, {"check_tensor", VFA_FUNCTION(check_tensor)},

@@ -534,3 +534,26 @@ def test_step_in_a_graph(vfa):
         assert all(torch.equal(a, b) for a, b in zip(*caches)), i
         lens += 1
         new += 1
+
+
+# ---- numbers past the range of their type ----------------------------------------------------------------------------------------
+
+def test_lengths_past_32_bits(vfa):
+    """A length or position that does not fit into an int is refused as one that does not fit into the cache is, not taken by its low bits."""
+    cache = vfa.kv8_cache(1, 2, 128, 64)
+    for t in cache:
+        t.zero_()
+    x, q = torch.ones((1, 2, 3, 64), dtype=torch.bfloat16, device="cuda"), torch.ones((1, 4, 64), dtype=torch.bfloat16, device="cuda")
+    before = [t.clone() for t in cache]
+    cs = torch.zeros((4, 64), device="cuda")
+    for big in (2 ** 31, 2 ** 32, 2 ** 32 + 3, 2 ** 40, -2 ** 32, -2 ** 63, 10 ** 30):
+        for f in (lambda: vfa.kv8_append(x, x, cache, 0, big), lambda: vfa.kv8_append(x, x, cache, big, big + 3), lambda: vfa.kv8_decode_fwd(q, cache, big),
+                  lambda: vfa.kv8_read(cache, 3, seq_lens=big), lambda: vfa.qk_norm_rope_fwd(x, x, cos_sin=cs, first_pos=big),
+                  lambda: vfa.kv8_decode_fwd(q, cache, 3, n_splits=2 ** 32 + 1)):
+            with pytest.raises(vfa.VfaError) as e:
+                f()
+            assert e.value.code == -1
+    one = x[:, :, :1].expand(1, 2, 2 ** 32, 64)
+    with pytest.raises(vfa.VfaError):
+        vfa.kv8_append(one, one, cache, ints([0]), ints([3]))
+    assert all(torch.equal(a, b) for a, b in zip(cache, before))
