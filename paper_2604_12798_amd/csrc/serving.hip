@@ -167,7 +167,7 @@ int vfa_kv8_read(const void* K8, const void* V8, const void* KS, const void* VS,
 // more than 16 rows make more of the merge (32 heads of 32 rows of 500 to 8192 keys: 4 ranges 16.9, 8 16.3, 16 19.4, 24 22.9).
 int vfa_kv8_decode_splits(int B, int Hq, int Hkv, int n_q, int d, int n_keys, int varlen) {
     if (B <= 0 || Hq <= 0 || Hkv <= 0 || n_q <= 0 || n_keys <= 0 || (long long)B * Hkv > 65535) return 1;
-    const int n_cu = cu_count() > 0 ? cu_count() : 256, all = ceil_div(n_keys, BN);
+    const int n_cu = cu_count() > 0 ? cu_count() : 256, all = n_keys / BN + (n_keys % BN != 0);  // (n_keys + 63 may not fit)
     const long long rows = (long long)(Hq / Hkv) * n_q;
     const int g = Hq / Hkv, tokens = rows <= 32 ? n_q : g < 32 ? 32 / g : 1;
     const long long heads = (long long)B * Hkv * (((long long)n_q + tokens - 1) / tokens);  // (with more than 32 rows, groups of them)

@@ -68,3 +68,15 @@ def test_numbers_past_the_range_of_their_type(p):
 class Ptr:
     def data_ptr(self):
         return 0x1000
+
+
+def test_suggested_ranges_at_the_end_of_the_type(p):
+    """Lengths above the largest that fits whole blocks into an int are as that."""
+    L = p.lib()
+    most = 2 ** 31 - 64
+    for B, Hq, Hkv, n_q in ((1, 8, 8, 1), (1, 32, 8, 1), (4, 32, 8, 1), (1, 32, 8, 4), (1, 32, 8, 64), (16, 32, 8, 1), (1, 1, 1, 1)):
+        for d in (64, 128):
+            for varlen in (0, 1):
+                want = L.vfa_kv8_decode_splits(B, Hq, Hkv, n_q, d, most, varlen)
+                for n in (most + 1, most + 2, 2 ** 31 - 1):
+                    assert L.vfa_kv8_decode_splits(B, Hq, Hkv, n_q, d, n, varlen) == want, (B, Hq, Hkv, n_q, d, varlen, n)
