@@ -536,6 +536,54 @@ def test_step_in_a_graph(vfa):
         new += 1
 
 
+# ---- values at the top of bf16 ---------------------------------------------------------------------------------------------------
+
+def top_block(c, b, t, seed):
+    """Block t of sequence b gets the largest exponent that writing gives, 120, and values of some 2^120."""
+    for h in range(c.codes[1].shape[1]):
+        g = torch.Generator().manual_seed(seed + h)
+        c.codes[1][b, h, 64 * t: 64 * t + 64] = ref.nearest(torch.randn((64, c.codes[1].shape[3]), generator=g, dtype=ref.F64))
+        c.exp[1][b, h, t] = 120
+
+
+@pytest.mark.parametrize("d,g,n_q", [(64, 2, 4), (128, 6, 4), (64, 5, 11), (128, 3, 30)])
+@pytest.mark.parametrize("n_splits", [1, 2])
+def test_top_of_bf16_in_a_draft(vfa, d, g, n_q, n_splits):
+    """Codes of 256 and 448 under 2^120, which bf16 would take for infinities, in the second and third of the last four new tokens: those before them
+    do not see them, and no other feature is spoiled for those who do."""
+    B, H, cap = 2, 1, 192
+    lens = [66, 140]
+    c = ref.random_cache(B, H, cap, d, 7)
+    for b, n in enumerate(lens):
+        for t in sorted({(n - 3) // 64, (n - 2) // 64}):
+            top_block(c, b, t, 10 * b + t)
+        c.codes[1][b, :, n - 3, 5] = 0x78
+        c.codes[1][b, :, n - 2, d - 1] = 0xfe
+    q = rows((B, g, n_q, d), 8, 0.4).cuda()
+    O, L = vfa.kv8_decode_fwd(q, ref.pack(c), ints(lens), n_splits=n_splits)
+    o, l, a = ref.attend(q, c.values(), lens)
+    first = n_q - 3  # (the first token that sees one)
+    ref.check(O[:, :, :first], L[:, :, :first], (o[:, :, :first], l[:, :, :first], a[:, :, :first]))
+    other = [f for f in range(d) if f not in (5, d - 1)]
+    ref.check(O[..., other], L, (o[..., other], l, a[..., other]))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n_q,n", [(1, 200), (3, 200), (20, 200), (1, 40)])
+def test_top_of_bf16_under_a_weight_of_zero(vfa, d, n_q, n):
+    """A key so far below the others that its weight is zero, with a value that bf16 would take for an infinity."""
+    c = ref.random_cache(1, 2, 256, d, 9)
+    c.codes[0].zero_()
+    c.codes[0][:, :, 10] = 0xfe  # -448
+    c.exp[0].zero_()
+    top_block(c, 0, 0, 3)
+    c.codes[1][0, :, 10, ::3] = 0x7e
+    q = torch.full((1, 4, n_q, d), 4.0, dtype=torch.bfloat16).cuda()
+    for ns in (1, 2):
+        O, L = vfa.kv8_decode_fwd(q, ref.pack(c), n, n_splits=ns)
+        ref.check(O, L, ref.attend(q, c.values(), [n]))
+
+
 # ---- numbers past the range of their type ----------------------------------------------------------------------------------------
 
 def test_lengths_past_32_bits(vfa):
