@@ -392,7 +392,8 @@ size_t vfa_kv8_decode_workspace_bytes(int B, int Hq, int n_q, int d, int n_split
 /* Attention of each sequence's n_q newest tokens (1: a decode step; more: drafted tokens, or a piece of a prompt) over its cache, which holds
  * them already.  Q, O [B, Hq, n_q, d] bf16, LSE [B, Hq, n_q] fp32 or NULL.  Sequence b has L = seq_lens[b] tokens (NULL: n_keys), and its token t of the
  * n_q sees the first L - n_q + 1 + t of them; a token that sees none (L < n_q) gets O = 0, LSE = -inf.  Exact attention over the values that
- * the cache stands for: products of bf16 queries with them and sums in fp32, softmax in fp32, weights rounded to bf16 for the product with V.
+ * the cache stands for: products of bf16 queries with them and sums in fp32, softmax in fp32; weights for the product with V to 2^-14 of each
+ * where a KV head has up to 8 rows (Hq / Hkv) * n_q, else rounded to bf16.  A key's value of 1.9375 * 2^127 and above counts as infinite.
  * Hq / Hkv <= 32, else VFA_ERR_UNSUPPORTED; up to 32 rows (Hq / Hkv) * n_q of a KV head are one workgroup's, more (a prompt in pieces) are cut into groups of whole
  * tokens, which read the cache each.  n_splits as in vfa_decode_varlen_fwd (1 to 4096; vfa_kv8_decode_splits suggests one);
  * the workspace, 16-byte aligned, contents irrelevant, is used for n_splits > 1 only.  Calls that may run at the same time need workspaces of their own. */

@@ -17,6 +17,11 @@ namespace {
 // Token t of the n_q sees keys < len - n_q + 1 + t.  What lies behind a sequence's end is neither a key (its scores are -inf) nor a value (its
 // codes are cleared: 0 * NaN).  A NaN in the value of a key that only some of the tokens see would reach the others through weights of zero: it is
 // cleared, too, and the sums of those who see it are set.
+// The product with V takes weights in bf16.  Up to eight rows leave half of a tile's columns free (HALVES): column c + 8 has the same row as c, and of each weight
+// c takes the upper 16 bits, c + 8 what they leave; their sums are added where the waves meet.  So a weight is held to 2^-14 for 34 more vector instructions a
+// tile of 250 (us: 2048 keys of 32 heads over 8 6.35 / 6.5, 4 x 32768 48.1 / 48.3, 128 heads of 100 to 2048 keys, d = 64, 9.35 / 9.55).  With more
+// rows the columns are taken, and a weight is rounded to bf16, 2^-8 of it at most, as in the bf16 decode: a second half would need a
+// tile of its own (16 rows 14.9 us, as 32 columns 16.2), and where the rows come in groups a half more products.  The sum that divides has the unrounded weights in fp32.
 // More than 32 rows (GROUPED: a prompt in pieces) are cut into groups of as many tokens as give 32, each with a workgroup of its own for each range; its last
 // token's keys take the place of the sequence's.  The KV heads come first in the grid, so that eights of them have an XCD each, in whose L2 their groups find the
 // tiles (groups first: 64 of 16384 tokens of 32 heads over 8 47 us, 32 now; 8 x 64 of 4096 81, 45), and the loads are not non-temporal.  The matrix unit is what
@@ -54,7 +59,7 @@ __device__ __forceinline__ void kv8_request(const uint8_t* base, int bytes, uint
     for (int u = 0; u < NI; ++u) r[u] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, off, u * 1024, NT ? 2 : 0));
 }
 
-template <int D, int RT, int W, int LENS, bool GROUPED = false>
+template <int D, int RT, int W, int LENS, bool GROUPED = false, bool HALVES = false>
 __global__ __launch_bounds__(64 * W, RT == 1 ? 3 : 2) void kv8_decode_kernel(const Kv8Decode P) {
     const DecodeParams& p = P.d;
     constexpr int S = D / 64, DT = D / 16, NI = D / 16, BYTES = BN * D;
@@ -93,7 +98,7 @@ __global__ __launch_bounds__(64 * W, RT == 1 ? 3 : 2) void kv8_decode_kernel(con
     int sees[RT];  // keys that the lane's rows see
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        const int row = min(16 * rt + ql, rows - 1);
+        const int row = min(HALVES ? ql & 7 : 16 * rt + ql, rows - 1);
         const uint16_t* const q = p.Q + ((size_t)b * p.Hq + row_of(row)) * D;
 #pragma unroll
         for (int s = 0; s < 2 * S; ++s) qf[rt][s] = *reinterpret_cast<const bf16x8*>(q + 64 * (s >> 1) + 16 * kg + 8 * (s & 1));
@@ -109,6 +114,8 @@ __global__ __launch_bounds__(64 * W, RT == 1 ? 3 : 2) void kv8_decode_kernel(con
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) ot[rt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    static_assert(!HALVES || RT == 1, "two columns of one tile for each row");
+    const uint32_t upper = ql >= 8 ? 0xffff0000u : 0u;  // HALVES: what a column leaves out of a weight
     u32x4 rk[NI], rv[NI];
     int sk = 0, sv = 0;
     auto want = [&](int t) { return t < r1 ? BYTES : 0; };
@@ -179,8 +186,15 @@ __global__ __launch_bounds__(64 * W, RT == 1 ? 3 : 2) void kv8_decode_kernel(con
                     e4[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[rt][kt][e], p.c, -msub));
                     lsum[rt] += e4[e];
                 }
-                pk[2 * kt] = pack_bf16(e4[0], e4[1]);
-                pk[2 * kt + 1] = pack_bf16(e4[2], e4[3]);
+                if (HALVES) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) e4[e] -= __uint_as_float(__float_as_uint(e4[e]) & upper);
+                    pk[2 * kt] = kv8_pair<true>(__float_as_uint(e4[0]), __float_as_uint(e4[1]));
+                    pk[2 * kt + 1] = kv8_pair<true>(__float_as_uint(e4[2]), __float_as_uint(e4[3]));
+                } else {
+                    pk[2 * kt] = pack_bf16(e4[0], e4[1]);
+                    pk[2 * kt + 1] = pack_bf16(e4[2], e4[3]);
+                }
             }
             pf[rt][0] = __builtin_bit_cast(bf16x8, u32x4{pk[0], pk[1], pk[2], pk[3]});
             pf[rt][1] = __builtin_bit_cast(bf16x8, u32x4{pk[4], pk[5], pk[6], pk[7]});
@@ -294,7 +308,9 @@ __global__ __launch_bounds__(64 * W, RT == 1 ? 3 : 2) void kv8_decode_kernel(con
         for (int v = 0; v < W; ++v) {
             const float a = __builtin_amdgcn_exp2f(ex[v * WS + 16 * RT * OROW + col] - msub);
             lt += a * ex[v * WS + 16 * RT * OROW + 16 * RT + col];
-            o += a * *reinterpret_cast<const f32x4*>(ex + v * WS + col * OROW + 4 * c4);
+            const float* const x = ex + v * WS + col * OROW + 4 * c4;
+            if (HALVES) o += a * (*reinterpret_cast<const f32x4*>(x) + *reinterpret_cast<const f32x4*>(x + 8 * OROW));
+            else o += a * *reinterpret_cast<const f32x4*>(x);
         }
         if (p.n_splits == 1) {  // the only range: this is the result
             const size_t row = (size_t)b * p.Hq + row_of(col);

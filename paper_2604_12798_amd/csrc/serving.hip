@@ -230,22 +230,24 @@ int vfa_kv8_decode_fwd(const void* Q, const void* K8, const void* V8, const void
         // takes as long for 2048 keys as one of 4, 13 us); d = 64 has half as much in a wave, and one long range eight waves (32 heads of 2048 keys
         // 9.9 / 8.2 us, 128 of 32768 119 / 94)
         const bool wide = D == 64 && n_splits == 1 && p.n_keys > 1024 && !grouped;
-        auto launch = [&](auto rt_c, auto w_c) {
+        auto launch = [&](auto rt_c, auto w_c, auto halves_c) {
             constexpr int RT = decltype(rt_c)::value, W = decltype(w_c)::value;
+            constexpr bool HALVES = decltype(halves_c)::value;
             const dim3 grid((unsigned)n_splits, (unsigned)B, (unsigned)Hkv);
             if constexpr (W == 4) {  // (one range is not dealt out)
                 if (dealt) {
-                    kv8_decode_kernel<D, RT, W, LENS_DEALT><<<grid, 64 * W, 0, s>>>(P);
+                    kv8_decode_kernel<D, RT, W, LENS_DEALT, false, HALVES><<<grid, 64 * W, 0, s>>>(P);
                     return;
                 }
             }
-            if (!seq_lens) kv8_decode_kernel<D, RT, W, LENS_ONE><<<grid, 64 * W, 0, s>>>(P);
-            else kv8_decode_kernel<D, RT, W, LENS_FIXED><<<dim3((unsigned)n_splits, (unsigned)Hkv, (unsigned)B), 64 * W, 0, s>>>(P);
+            if (!seq_lens) kv8_decode_kernel<D, RT, W, LENS_ONE, false, HALVES><<<grid, 64 * W, 0, s>>>(P);
+            else kv8_decode_kernel<D, RT, W, LENS_FIXED, false, HALVES><<<dim3((unsigned)n_splits, (unsigned)Hkv, (unsigned)B), 64 * W, 0, s>>>(P);
         };
         using std::integral_constant;
         auto sized = [&](auto w_c) {
-            if (rows <= 16) launch(integral_constant<int, 1>{}, w_c);
-            else launch(integral_constant<int, 2>{}, w_c);
+            if (rows <= 8) launch(integral_constant<int, 1>{}, w_c, std::true_type{});
+            else if (rows <= 16) launch(integral_constant<int, 1>{}, w_c, std::false_type{});
+            else launch(integral_constant<int, 2>{}, w_c, std::false_type{});
         };
         if (grouped) {
             const dim3 grid((unsigned)Hkv, (unsigned)(groups * n_splits), (unsigned)B);

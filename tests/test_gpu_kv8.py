@@ -605,3 +605,24 @@ def test_lengths_past_32_bits(vfa):
     with pytest.raises(vfa.VfaError):
         vfa.kv8_append(one, one, cache, ints([0]), ints([3]))
     assert all(torch.equal(a, b) for a, b in zip(cache, before))
+
+
+# ---- weights ---------------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("g,n_q", [(1, 1), (4, 1), (8, 1), (1, 8), (2, 3), (7, 1)])
+@pytest.mark.parametrize("n_splits", [1, 3])
+def test_weights_of_up_to_eight_rows(vfa, d, g, n_q, n_splits):
+    """Up to eight rows of a KV head have their weights in two halves of bf16, 2^-14 of each in all.  Scores are sums of d products in 32 bits (2^-17 of the
+    terms' size, in the weight and in the sum that divides it), the rest (exponentials, sums of up to 130 keys) below 2^-16; O is rounded once."""
+    lens = [1, 2, 3, 4, 5, 9, 17, 64, 65, 130]
+    B, H, cap = len(lens), 2, 192
+    c = ref.random_cache(B, H, cap, d, d + g)
+    q = rows((B, g * H, n_q, d), n_q, 0.2).cuda()
+    O, L = vfa.kv8_decode_fwd(q, ref.pack(c), ints(lens), n_splits=n_splits)
+    K, V = c.values()
+    o, l, a = ref.attend(q, [K, V], lens)
+    terms = (q.double().cpu().abs().reshape(B, H, -1, d) @ K.abs().transpose(2, 3)).amax().item() * d ** -0.5
+    off = (O.double().cpu() - o).abs() - (2.0 ** -14 + 2.0 ** -16 * (1 + terms)) * a - 2.0 ** -8 * o.abs()
+    assert terms < 16 and (off <= 0).all(), (terms, off.max().item())
+    ref.check(O, L, (o, l, a))
