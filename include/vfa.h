@@ -360,7 +360,7 @@ int vfa_mxfp4_attn_noexp_fwd(const void* Q4, const void* QS, const void* K4, con
  * (i, i + rot_dim / 2) or, interleaved = 1, (2 i, 2 i + 1):  y_a = z_a cos - z_b sin, y_b = z_b cos + z_a sin, with cos and sin of the token's
  * position from cos_sin [n_pos, rot_dim] fp32 (16-byte aligned; a row holds rot_dim / 2 cosines, then as many sines).  Token n of entry b has
  * position first_pos[b] + n (DEVICE array; NULL: first + n), clamped to [0, n_pos - 1].  Values are copied.
- * Computed in fp32 from the bf16 inputs, rounded to bf16 once. */
+ * Computed in fp32 from the bf16 inputs, rounded to bf16 once (a row whose sum of squares is past fp32's range, elements of some 10^18, gives zeros). */
 int vfa_qk_norm_rope_fwd(const void* Xq, const void* Xk, const void* Xv, void* Q, void* K, void* V, int B, int N,
                          int Hq, int Hkv, int d, long long q_sb, long long q_sn, long long q_sh, long long k_sb,
                          long long k_sn, long long k_sh, long long v_sb, long long v_sn, long long v_sh, int norm,

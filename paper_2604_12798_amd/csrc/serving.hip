@@ -93,8 +93,8 @@ int vfa_qk_norm_rope_fwd(const void* Xq, const void* Xk, const void* Xv, void* Q
         auto sized = [&](auto norm_c) {
             using std::integral_constant;
             if (few) launch(norm_c, integral_constant<int, 1>{}, std::false_type{});
-            else if (stream_past) launch(norm_c, integral_constant<int, 4>{}, std::true_type{});
-            else launch(norm_c, integral_constant<int, 4>{}, std::false_type{});
+            else if (!stream_past) launch(norm_c, integral_constant<int, 4>{}, std::false_type{});
+            else if constexpr (D == 128) launch(norm_c, integral_constant<int, 4>{}, std::true_type{});
         };
         if (norm) sized(std::true_type{});
         else sized(std::false_type{});
@@ -155,16 +155,18 @@ int vfa_kv8_read(const void* K8, const void* V8, const void* KS, const void* VS,
     return launched();
 }
 
-// One range for each KV head, which is one launch and no partial sums, where there are few keys, and more of them the more units the heads fill (us, one range /
-// the best number of ranges; d = 128: 8 heads of 768 keys 6.1 / 6.8, of 1024 7.0 / 6.5, of 1536 10.2 / 7.2; 128 of 1536 12.2 / 12.8, of 200 to 2048 14.1 / 13.1;
-// 256 of 100 to 1024 10.2 / 13.5, of 200 to 2048 16.6 / 18.7, of 200 to 4096 29.9 / 29.9; d = 64: 16 of 1024 5.2 / 6.5, of 2048 9.9 / 6.7; 128 of 100 to 2048
-// 8.6 / 10.0; 256 of as many 10.0 / 12.8, 288 of 300 to 6175 25.5 / 26.8).
+// One range for each KV head, which is one launch and no partial sums, where there are few keys, and more of them the more units the heads fill; the limits lie
+// where the two meet (us, one range / the best number of ranges; d = 128: 8 heads of 768 keys 6.1 / 6.8, of 1024 7.0 / 6.5, of 1536 10.2 / 7.2; 128 of 1536
+// 12.2 / 12.8, of 200 to 2048 14.1 / 13.1; 256 of 100 to 1024 10.2 / 13.5, of 200 to 4096 28.5 / 28.8, to 5120 36.1 / 33.9; d = 64: 16 of 1024 5.2 / 6.5, of
+// 2048 9.9 / 6.7; 128 of 100 to 2048 8.6 / 10.0, to 2560 10.2 / 10.5, to 3200 12.0 / 11.2; 256 of 100 to 2048 10.0 / 12.8, to 6208 23.1 / 23.8, to 8192
+// 29.7 / 27.9; 288 of 300 to 6144 26.0 / 26.6, to 6175 26.9 / 26.2, to 8192 34.6 / 31.9).
 // Else as many workgroups as there are compute units where all are equally long: a unit has 64 KiB on their way to it in either case, and fewer
 // partial sums (32 heads of 32768 keys, d = 128: 8 ranges 45.0, 12 46.8, 16 49.5, 24 45.7; 128 of 4224: 1 27.0, 2 26.0, 3 27.0, 6 25.8; d = 64, 128 of
 // 32768: 1 119, 2 80, 3 85, 6 83).  Where lengths differ and ranges are dealt out, as many as the units hold at a time, three each, so that what a range is
 // longer than the mean weighs less (128 heads of 200 to 8192 keys: 2 ranges 30.2, 4 29.0, 6 27.8, 8 29.9; 512 of 200 to 2048: 1 29.1, 2 33.2; more fit
-// in at d = 64, 288 heads of 300 to 6175 keys: 2 30.2, 3 26.9, 4 26.8), but one where
-// more than 16 rows make more of the merge (32 heads of 32 rows of 500 to 8192 keys: 4 ranges 16.9, 8 16.3, 16 19.4, 24 22.9).
+// in at d = 64, 288 heads of 300 to 6175 keys: 2 30.1, 3 28.3, 4 26.2), but one where
+// more than 16 rows make more of the merge (32 heads of 500 to 8192 keys, 32 rows each: 4 ranges 18.1, 8 16.1, 16 19.4, 24 22.5; 20 rows: 16.7, 14.5, 16.5,
+// 21.2; 64 heads, 24 rows, d = 64: 2 18.6, 4 13.7, 8 14.7, 16 20.0).
 int vfa_kv8_decode_splits(int B, int Hq, int Hkv, int n_q, int d, int n_keys, int varlen) {
     if (B <= 0 || Hq <= 0 || Hkv <= 0 || n_q <= 0 || n_keys <= 0 || (long long)B * Hkv > 65535) return 1;
     const int n_cu = cu_count() > 0 ? cu_count() : 256, all = n_keys / BN + (n_keys % BN != 0);  // (n_keys + 63 may not fit)
