@@ -24,8 +24,9 @@ namespace {
 // tile of its own (16 rows 14.9 us, as 32 columns 16.2), and where the rows come in groups a half more products.  The sum that divides has the unrounded weights in fp32.
 // More than 32 rows (GROUPED: a prompt in pieces) are cut into groups of as many tokens as give 32, each with a workgroup of its own for each range; its last
 // token's keys take the place of the sequence's.  The KV heads come first in the grid, so that eights of them have an XCD each, in whose L2 their groups find the
-// tiles (groups first: 64 of 16384 tokens of 32 heads over 8 47 us, 32 now; 8 x 64 of 4096 81, 45), and the loads are not non-temporal.  The matrix unit is what
-// bounds them: D = 128, the last 1024 of 16384 tokens 300 us (887 TFLOP/s), all of 2 x 16384 4.55 ms (967).
+// tiles (groups first: 64 of 16384 tokens of 32 heads over 8 47 us, 33 now; 8 x 64 of 4096 81, 49), and the loads are not non-temporal.  Their vector
+// instructions are what bounds them, since every wave converts its tiles for 32 rows only: D = 128, the last 1024 of 16384 tokens 288 us (924 TFLOP/s), the vector unit
+// busy 75 % of the time and the matrix unit 44 %, two fifths of that together; 256 of them 89 us, 70 and 39 %; all of 2 x 16384 4.74 ms (928 TFLOP/s).
 // Partial sums of ranges and their merge: decode.hpp, a row for a head.
 struct Kv8Decode {
     DecodeParams d;  // Hq, g: rows for heads (query heads times new tokens); K, V not used
