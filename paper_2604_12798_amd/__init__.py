@@ -150,11 +150,11 @@ def _on(stream, f, args):
     """f(**args) with its `stream` as the current one, for a wrapper that allocates.  Memory for a call on another stream has to be that stream's: in what the
     current stream gives out, work of its own may still be under way, and a workspace that is dropped at the return would be given out again while the call
     runs.  Outputs are used on the stream that was current, so they are kept from others until that one is through with them, too."""
-    import torch
     args["stream"] = None
-    before = torch.cuda.current_stream()
-    if stream == before:
+    if stream.cuda_stream == _stream(None) and stream.device_index == _current_device():
         return f(**args)
+    import torch
+    before = torch.cuda.current_stream()
     with torch.cuda.stream(stream):
         out = f(**args)
     given = [x for a in args.values() for x in (a if isinstance(a, (tuple, list)) else (a,))]

@@ -21,6 +21,8 @@ BF, U8, I32, F32 = torch.bfloat16, torch.uint8, torch.int32, torch.float32
 
 
 class Stream:
+    device_index = 0
+
     def __init__(self, handle):
         self.cuda_stream = handle
 
