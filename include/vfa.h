@@ -401,6 +401,64 @@ int vfa_kv8_decode_fwd(const void* Q, const void* K8, const void* V8, const void
                        int B, int Hq, int Hkv, int n_cap, int n_q, int d, const int* seq_lens, int n_keys, int n_splits,
                        float softmax_scale, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- Serving from a paged bf16 cache, and prompts whose scores are capped, biased or masked by more than causality.  A prompt takes vfa_row_ranges (if
+ * it is packed or has prefixes), vfa_masked_attn_fwd and vfa_kvp_append; a step vfa_kvp_append and vfa_kvp_decode_fwd.  Only d in {64, 128}.  None of
+ * these calls sets a function attribute: each may be captured first.
+ *
+ * Scores.  s = softmax_scale * q . k (softmax_scale <= 0: 1 / sqrt(d)); with score_cap > 0 it becomes score_cap * tanh(s / score_cap); with slopes,
+ * fp32 [Hq] on the device, slopes[h] * |distance between the positions of row and key| is subtracted from that.  score_cap is 0 (none) or 0.001 to 1000.
+ * Scores and sums are held in fp32 (a cap's error is 2^-22 of it, which is an error of the exponents).
+ *
+ * The cache is a pool of pages, KP, VP [n_pages, Hkv, page, d] bf16 (page a power of two, 16 or more, else VFA_ERR_UNSUPPORTED; 16-byte aligned),
+ * and a table, int32 [B, max_pages] on the device: token n of sequence b lies in page table[b][n / page], row n % page.  max_pages * page <= 2^30.  An
+ * entry outside [0, n_pages) is a hole: nothing is written there, and its tokens are seen by nobody.  So a table may hold anything behind a sequence's end, and
+ * a page whose tokens are to be forgotten may be taken out.  Sequences may share pages that are only read.  Lengths are one for all (ints), or
+ * DEVICE arrays of B ints, 4-byte aligned, clamped to [0, max_pages * page].  B * Hkv <= 65535. ---- */
+
+/* Writes new rows into the pages: sequence b gets rows 0, 1, ... of K, V [B, Hkv, n_in, d] (bf16, any strides in elements, multiples of 8: batch,
+ * head, token) as its tokens old_lens[b] <= n < new_lens[b] (n_in of them at most; none where old >= new), or all sequences as n_old <= n < n_new (both
+ * arrays NULL; VFA_ERR_INVALID_ARG unless 0 <= n_old <= n_new <= max_pages * page and n_new - n_old <= n_in).  All other rows of the pool stay as they are.  Two
+ * sequences that write the same row of a page race. */
+int vfa_kvp_append(const void* K, const void* V, void* KP, void* VP, const int* table, int B, int Hkv, int n_pages, int page,
+                   int max_pages, int n_in, int d, long long k_sb, long long k_sh, long long k_sn, long long v_sb,
+                   long long v_sh, long long v_sn, const int* old_lens, const int* new_lens, int n_old, int n_new,
+                   void* stream);
+
+/* A number of key ranges for vfa_kvp_decode_fwd that suits a batch of sequences of n_keys tokens each (varlen = 0), or of lengths of their own up to
+ * n_keys (varlen = 1), on the current device. */
+int vfa_kvp_decode_splits(int B, int Hq, int Hkv, int n_q, int d, int n_keys, int varlen);
+
+/* Bytes of workspace vfa_kvp_decode_fwd needs for n_splits > 1. */
+size_t vfa_kvp_decode_workspace_bytes(int B, int Hq, int n_q, int d, int n_splits);
+
+/* Attention of each sequence's n_q newest tokens (1: a decode step; more: drafted tokens, or a piece of a prompt) over its pages, which hold them
+ * already.  Q, O [B, Hq, n_q, d] bf16, LSE [B, Hq, n_q] fp32 or NULL.  Sequence b has L = seq_lens[b] tokens (NULL: n_keys); its token t of the n_q has
+ * position L - n_q + t and sees the keys up to that one; a token that sees none gives O = 0, LSE = -inf.  What a row does not see does not reach it,
+ * infinities and NaN among the values included.  Weights for the product with V are held to 2^-16 where a KV head has up to 16 rows (Hq / Hkv) * n_q, else
+ * rounded to bf16.  Hq / Hkv <= 32, else VFA_ERR_UNSUPPORTED; up to 32 rows of a KV head are one workgroup's, more (a prompt in pieces) are cut into groups
+ * of whole tokens, which read the pages each.  n_splits and workspace as in vfa_kv8_decode_fwd (1 to 4096; vfa_kvp_decode_splits suggests one; the
+ * workspace, 16-byte aligned, contents irrelevant, is used for n_splits > 1 only).  Calls that may run at the same time need workspaces of their own. */
+int vfa_kvp_decode_fwd(const void* Q, const void* KP, const void* VP, const int* table, void* O, float* LSE, int B, int Hq,
+                       int Hkv, int n_pages, int page, int max_pages, int n_q, int d, const int* seq_lens, int n_keys,
+                       int n_splits, float softmax_scale, float score_cap, const float* slopes, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/* The keys that each row of a packed batch sees, ranges [B, N, 2] int32 (8-byte aligned): first key, and the one behind the last.  Document k of entry b holds
+ * the rows doc_offsets[b][k] <= i < doc_offsets[b][k + 1] (int32 [B, n_docs + 1] on the device, not decreasing, clamped to [0, N]; documents may be
+ * empty).  Its rows see the document's keys: all of them (causal = 0), or up to themselves, and all of its first prefix_lens[b][k] ones (causal = 1;
+ * int32 [B, n_docs], NULL: no prefixes; not read for causal = 0).  Rows outside of all documents (before the first, padding behind the last) see nothing: 0, 0. */
+int vfa_row_ranges(const int* doc_offsets, const int* prefix_lens, int* ranges, int B, int N, int n_docs, int causal,
+                   void* stream);
+
+/* Attention of whole prompts.  Layouts as above (Q, O [B, Hq, N, d], K, V [B, Hkv, N, d], LSE may be NULL).  Row i of entry b sees the keys
+ * ranges[b][i][0] <= j < ranges[b][i][1] (int32 [B, N, 2] on the device, 8-byte aligned, from vfa_row_ranges or any others, e.g. windows; clamped to [0, N];
+ * NULL: all keys) and, with causal = 1, of those the ones up to itself; a row that sees none gives O = 0, LSE = -inf.  Positions are i and j.  What a
+ * row does not see does not reach it, infinities and NaN included.  Exact attention; weights are rounded to bf16 for the product with V, as in vfa_attn_fwd.  2 * d * N
+ * < 2^31, else VFA_ERR_UNSUPPORTED. */
+int vfa_masked_attn_fwd(const void* Q, const void* K, const void* V, void* O, float* LSE, int B, int Hq, int Hkv, int N, int d,
+                        int causal, const int* ranges, float softmax_scale, float score_cap, const float* slopes,
+                        void* stream);
+
 /* Static string for a return code. */
 const char* vfa_strerror(int code);
 

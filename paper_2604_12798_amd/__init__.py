@@ -20,7 +20,8 @@ EXPORTS = ("vfa_workspace_bytes", "vfa_kblock_summary", "vfa_kblock_summary_mode
            "fa_lazy_rescale_fwd", "fa_lazy_rescale_softexp_fwd", "vfa_attn_fwd", "vsa_attn_fwd", "vfa_variant_fwd", "vfa_kblock_summary_append",
            "vfa_decode_workspace_bytes", "vfa_decode_fwd", "vfa_decode_noalloc_fwd", "vfa_kblock_summary_append_varlen", "vfa_decode_varlen_fwd", "vfa_fp8_quantize", "vfa_fp8_v_bytes", "vfa_fp8_pack_v",
            "vfa_fp8_attn_fwd", "vfa_fp8_attn_noexp_fwd", "vfa_mxfp4_quantize", "vfa_mxfp4_workspace_bytes", "vfa_mxfp4_attn_fwd", "vfa_mxfp4_attn_noexp_fwd", "vfa_strerror",
-           "vfa_qk_norm_rope_fwd", "vfa_kv8_append", "vfa_kv8_read", "vfa_kv8_decode_splits", "vfa_kv8_decode_workspace_bytes", "vfa_kv8_decode_fwd")
+           "vfa_qk_norm_rope_fwd", "vfa_kv8_append", "vfa_kv8_read", "vfa_kv8_decode_splits", "vfa_kv8_decode_workspace_bytes", "vfa_kv8_decode_fwd",
+           "vfa_kvp_append", "vfa_kvp_decode_splits", "vfa_kvp_decode_workspace_bytes", "vfa_kvp_decode_fwd", "vfa_row_ranges", "vfa_masked_attn_fwd")
 
 
 class VfaError(RuntimeError):
@@ -104,6 +105,18 @@ def lib() -> ctypes.CDLL:
         L.vfa_kv8_decode_workspace_bytes.argtypes = [i, i, i, i, i]
         L.vfa_kv8_decode_fwd.restype = i
         L.vfa_kv8_decode_fwd.argtypes = [vp] * 7 + [i] * 6 + [vp, i, i, f, vp, sz, vp]
+        L.vfa_kvp_append.restype = i
+        L.vfa_kvp_append.argtypes = [vp] * 5 + [i] * 7 + [ll] * 6 + [vp, vp, i, i, vp]
+        L.vfa_kvp_decode_splits.restype = i
+        L.vfa_kvp_decode_splits.argtypes = [i] * 7
+        L.vfa_kvp_decode_workspace_bytes.restype = sz
+        L.vfa_kvp_decode_workspace_bytes.argtypes = [i] * 5
+        L.vfa_kvp_decode_fwd.restype = i
+        L.vfa_kvp_decode_fwd.argtypes = [vp] * 6 + [i] * 8 + [vp, i, i, f, f, vp, vp, sz, vp]
+        L.vfa_row_ranges.restype = i
+        L.vfa_row_ranges.argtypes = [vp] * 3 + [i] * 4 + [vp]
+        L.vfa_masked_attn_fwd.restype = i
+        L.vfa_masked_attn_fwd.argtypes = [vp] * 5 + [i] * 6 + [vp, f, f, vp, vp]
         _lib = L
     return _lib
 
@@ -640,4 +653,117 @@ def kv8_decode_fwd(q, cache, seq_lens, *, n_splits=None, softmax_scale=0.0, work
                                 workspace, ws_bytes, _stream(stream))
     if rc != 0:
         raise VfaError(rc, "vfa_kv8_decode_fwd")
+    return out, lse
+
+
+def kvp_cache(n_pages: int, Hkv: int, page: int, d: int, device=None):
+    """A pool of pages for a paged cache: (KP, VP) [n_pages, Hkv, page, d] bf16 of vfa.h, not initialised (page: tokens, a power of two, 16 or more).
+    device: the current GPU if not given.  Which page holds which tokens of which sequence is the caller's table, int32 [B, max_pages]."""
+    import torch
+    dev = "cuda" if device is None else device
+    return tuple(torch.empty((n_pages, Hkv, page, d), dtype=torch.bfloat16, device=dev) for _ in range(2))
+
+
+def kvp_append(K, V, cache, table, old_lens, new_lens, stream=None):
+    """Writes rows of K, V [B, Hkv, n_in, d] (bf16, any strides) into the pages, in place, as tokens old_lens <= n < new_lens of each sequence (numbers, or
+    int32 tensors of B entries, both alike).  Entries of the table outside the pool take nothing."""
+    n = _ns()
+    KP, VP = cache
+    dev, *sizes = n.check_kvp_append(K, V, KP, VP, table, old_lens, new_lens, _bf16, _i32)
+    _serving(dev)
+    rc = n.vfa_kvp_append_t(K, V, KP, VP, table, *sizes, _stream(stream))
+    if rc != 0:
+        raise VfaError(rc, "vfa_kvp_append")
+    return cache
+
+
+def kvp_decode_workspace_bytes(B: int, Hq: int, n_q: int, d: int, n_splits: int) -> int:
+    return int(_n().vfa_kvp_decode_workspace_bytes(B, Hq, n_q, d, n_splits))
+
+
+def kvp_decode_splits(B: int, Hq: int, Hkv: int, n_q: int, d: int, n_keys: int, varlen: bool = False) -> int:
+    """Key ranges that suit a batch of n_keys tokens each, or (varlen) of lengths of their own up to n_keys."""
+    return int(_n().vfa_kvp_decode_splits(B, Hq, Hkv, n_q, d, n_keys, int(bool(varlen))))
+
+
+def kvp_decode_fwd(q, cache, table, seq_lens, *, score_cap=0.0, slopes=None, n_splits=None, softmax_scale=0.0, workspace=None, out=None, lse=None,
+                   want_lse=True, stream=None):
+    """Attention of each sequence's newest tokens, q [B, Hq, n_q, d] (or [B, Hq, d] for one), over the pages that hold them already: a step, drafts, a piece of
+    a prompt; seq_lens: a number or an int32 tensor of B entries.  score_cap: scores become score_cap * tanh(s / score_cap); slopes (fp32 [Hq]): slope times
+    distance is subtracted.  n_splits: key ranges (None: vfa_kvp_decode_splits, of the table's capacity where the lengths are on the GPU).  A workspace of
+    kvp_decode_workspace_bytes is for calls that must not allocate."""
+    if stream is not None and (out is None or workspace is None or (lse is None and want_lse)):
+        return _on(stream, kvp_decode_fwd, locals())
+    n = _ns()
+    KP, VP = cache
+    dev, B, Hq, Hkv, n_pages, page, max_pages, n_q, d, lens, n_keys = n.check_kvp_decode(q, KP, VP, table, seq_lens, slopes, _bf16, _f32, _i32)
+    _serving(dev)
+    if n_splits is None:
+        n_splits = n.vfa_kvp_decode_splits(B, Hq, Hkv, n_q, d, n_keys if lens is None else max_pages * page, int(lens is not None))
+    n_splits = int(n_splits)
+    if out is None:
+        out = _empty_like(q)
+    else:
+        _need(n.check_tensor(out, _bf16, dev, *q.shape), "out must be a contiguous bf16 tensor of q's shape on the same GPU")
+    if lse is not None:
+        _need(n.check_tensor(lse, _f32, dev, *q.shape[:-1]), "lse must be a contiguous fp32 tensor of q's shape without d on the same GPU")
+    elif want_lse:
+        lse = q.new_empty((B, Hq, n_q) if q.dim() == 4 else (B, Hq), dtype=_f32)
+    ws_bytes = 0
+    if n_splits > 1:
+        if workspace is None:
+            ws_bytes = n.vfa_kvp_decode_workspace_bytes(B, Hq, n_q, d, n_splits)
+            workspace = q.new_empty((ws_bytes,), dtype=_u8)
+        else:
+            _need(workspace.get_device() == dev and workspace.is_contiguous(), "the workspace must be a contiguous tensor on the same GPU")
+            ws_bytes = n.bytes_of(workspace)
+    rc = n.vfa_kvp_decode_fwd_t(q, KP, VP, table, out, lse, B, Hq, Hkv, n_pages, page, max_pages, n_q, d, lens, n_keys, n_splits, float(softmax_scale),
+                                float(score_cap), slopes, workspace, ws_bytes, _stream(stream))
+    if rc != 0:
+        raise VfaError(rc, "vfa_kvp_decode_fwd")
+    return out, lse
+
+
+def row_ranges(doc_offsets, N: int, *, prefix_lens=None, causal=True, out=None, stream=None):
+    """The keys that each row of a packed batch sees, int32 [B, N, 2] (the first, and the one behind the last), for masked_attn_fwd: document k of an entry
+    has the rows doc_offsets[k] <= i < doc_offsets[k + 1] (int32 [B, n_docs + 1]), whose first prefix_lens[k] (int32 [B, n_docs]) see each other both
+    ways and the others what is before them (causal), or which all see each other.  Rows outside of all documents see nothing."""
+    if stream is not None and out is None:
+        return _on(stream, row_ranges, locals())
+    n = _ns()
+    dev, B, n_docs = n.check_row_ranges(doc_offsets, prefix_lens, _i32)
+    _serving(dev)
+    N = int(N)
+    _need(N >= 0, "N must not be negative")
+    if out is None:
+        out = doc_offsets.new_empty((B, N, 2))
+    else:
+        _need(n.check_tensor(out, _i32, dev, B, N, 2), "out must be a contiguous int32 tensor [B, N, 2] on the same GPU")
+    rc = n.vfa_row_ranges_t(doc_offsets, prefix_lens, out, B, N, n_docs, int(bool(causal)), _stream(stream))
+    if rc != 0:
+        raise VfaError(rc, "vfa_row_ranges")
+    return out
+
+
+def masked_attn_fwd(Q, K, V, *, causal=None, ranges=None, score_cap=0.0, slopes=None, softmax_scale=0.0, out=None, lse=None, want_lse=True, stream=None):
+    """Attention of whole prompts, Q [B, Hq, N, d], K and V [B, Hkv, N, d].  ranges (int32 [B, N, 2], see row_ranges): the keys that each row sees; causal: only
+    those up to itself (None: causal where there are no ranges, which say all there is to say elsewhere).  score_cap: scores become score_cap * tanh(s /
+    score_cap); slopes (fp32 [Hq]): slope times distance is subtracted.  Returns (O, LSE); rows that see nothing give 0 and -inf."""
+    if stream is not None and (out is None or (lse is None and want_lse)):
+        return _on(stream, masked_attn_fwd, locals())
+    n = _ns()
+    dev, B, Hq, Hkv, N, d = n.check_masked_attn(Q, K, V, ranges, slopes, _bf16, _f32, _i32)
+    _serving(dev)
+    if out is None:
+        out = _empty_like(Q)
+    else:
+        _need(n.check_tensor(out, _bf16, dev, B, Hq, N, d), "out must be a contiguous bf16 tensor of Q's shape on the same GPU")
+    if lse is not None:
+        _need(n.check_tensor(lse, _f32, dev, B, Hq, N), "lse must be a contiguous fp32 tensor [B, Hq, N] on the same GPU")
+    elif want_lse:
+        lse = Q.new_empty((B, Hq, N), dtype=_f32)
+    rc = n.vfa_masked_attn_fwd_t(Q, K, V, out, lse, B, Hq, Hkv, N, d, int(ranges is None if causal is None else bool(causal)), ranges, float(softmax_scale),
+                                 float(score_cap), slopes, _stream(stream))
+    if rc != 0:
+        raise VfaError(rc, "vfa_masked_attn_fwd")
     return out, lse

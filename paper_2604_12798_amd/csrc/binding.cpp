@@ -365,6 +365,100 @@ PyObject* check_norm_rope(PyObject*, PyObject* const* args, Py_ssize_t n) {
     return Py_BuildValue("(lLLLLLLLLLLLLLLLLOO)", device, q[0], q[1], q[2], k[2], q[3], qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], table[0],
                          table[1], first.at, first.number);
 }
+// KP, VP and the table of a paged cache; (n_pages, Hkv, page, d) go to c, (B, max_pages) to t
+int pages(PyObject* const* args, PyObject* bf16, PyObject* int32, long& device, long long* c, long long* t) {
+    long long v[4];
+    int ok = whole_tensor(args[0], bf16, device, 4, c);
+    if (ok == 1) ok = whole_tensor(args[1], bf16, device, 4, v);
+    if (ok == 1) ok = whole_tensor(args[2], int32, device, 2, t);
+    for (int i = 0; ok == 1 && i < 4; ++i) ok = v[i] == c[i];
+    return ok;
+}
+const char kSlopes[] = "slopes must be a contiguous fp32 tensor of an entry for each query head on the same GPU";
+const char kPages[] = "a paged cache is two contiguous bf16 tensors [n_pages, Hkv, page, d] and a contiguous int32 table [B, max_pages], all on one GPU";
+
+// check_kvp_append(K, V, KP, VP, table, old, new, bfloat16, int32) -> (device, B, Hkv, n_pages, page, max_pages, n_in, d, strides of K, strides of V,
+// old_lens, new_lens, n_old, n_new)
+PyObject* check_kvp_append(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 9) return PyErr_Format(PyExc_TypeError, "expected 9 arguments, got %zd", n);
+    long device = -1;
+    long long c[4], t[2], k[4], v[4], ks[4], vs[4];
+    int ok = pages(args + 2, args[7], args[8], device, c, t);
+    if (ok != 1) return refused(ok, kPages);
+    ok = rows_tensor(args[0], args[7], device, k, ks);
+    if (ok == 1) ok = rows_tensor(args[1], args[7], device, v, vs);
+    if (ok == 1) ok = k[0] == t[0] && k[1] == c[1] && k[3] == c[3] && v[0] == k[0] && v[1] == k[1] && v[2] == k[2] && v[3] == k[3];
+    if (ok != 1) return refused(ok, "K, V must be bf16 tensors [B, Hkv, n_in, d] matching the cache and on its GPU, their last dimension contiguous");
+    Lengths o, m;
+    ok = o.set(args[5], args[8], device, t[0]);
+    if (ok == 1) ok = m.set(args[6], args[8], device, t[0]);
+    if (ok == 1) ok = (o.at == Py_None) == (m.at == Py_None);
+    if (ok != 1) return refused(ok, "old_lens and new_lens are both numbers, or both contiguous int32 tensors of an entry for each sequence on the same GPU");
+    return Py_BuildValue("(lLLLLLLLLLLLLLOOOO)", device, t[0], c[1], c[0], c[2], t[1], k[2], c[3], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], o.at, m.at,
+                         o.number, m.number);
+}
+// check_kvp_decode(q, KP, VP, table, lengths, slopes or None, bfloat16, float32, int32) -> (device, B, Hq, Hkv, n_pages, page, max_pages, n_q, d, seq_lens, n_keys)
+PyObject* check_kvp_decode(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 9) return PyErr_Format(PyExc_TypeError, "expected 9 arguments, got %zd", n);
+    long device = -1;
+    long long c[4], t[2], q[4] = {0, 0, 1, 0}, s[1];
+    int ok = pages(args + 1, args[6], args[8], device, c, t);
+    if (ok != 1) return refused(ok, kPages);
+    const Ref dims = method(args[0], names.dim);
+    const long nd = dims.o ? PyLong_AsLong(dims.o) : -1;
+    if (nd == -1 && PyErr_Occurred()) return nullptr;
+    ok = nd == 3 || nd == 4;
+    if (ok == 1) ok = whole_tensor(args[0], args[6], device, nd, q);
+    if (ok == 1 && nd == 3) { q[3] = q[2]; q[2] = 1; }
+    if (ok == 1) ok = q[0] == t[0] && q[3] == c[3];
+    if (ok != 1) return refused(ok, "q must be a contiguous bf16 tensor [B, Hq, n_q, d] or [B, Hq, d] matching the cache and on its GPU");
+    if (args[5] != Py_None) {
+        ok = whole_tensor(args[5], args[7], device, 1, s);
+        if (ok == 1) ok = s[0] == q[1];
+        if (ok != 1) return refused(ok, kSlopes);
+    }
+    Lengths l;
+    ok = l.set(args[4], args[8], device, t[0]);
+    if (ok != 1) return refused(ok, kLengths);
+    return Py_BuildValue("(lLLLLLLLLOO)", device, t[0], q[1], c[1], c[0], c[2], t[1], q[2], q[3], l.at, l.number);
+}
+// check_row_ranges(doc_offsets, prefix_lens or None, int32) -> (device, B, n_docs)
+PyObject* check_row_ranges(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 3) return PyErr_Format(PyExc_TypeError, "expected 3 arguments, got %zd", n);
+    long device = -1;
+    long long o[2], x[2];
+    int ok = whole_tensor(args[0], args[2], device, 2, o);
+    if (ok == 1) ok = o[1] >= 1;
+    if (ok != 1) return refused(ok, "doc_offsets must be a contiguous int32 tensor [B, n_docs + 1] on a GPU");
+    if (args[1] != Py_None) {
+        ok = whole_tensor(args[1], args[2], device, 2, x);
+        if (ok == 1) ok = x[0] == o[0] && x[1] == o[1] - 1;
+        if (ok != 1) return refused(ok, "prefix_lens must be a contiguous int32 tensor [B, n_docs] on the same GPU");
+    }
+    return Py_BuildValue("(lLL)", device, o[0], o[1] - 1);
+}
+// check_masked_attn(Q, K, V, ranges or None, slopes or None, bfloat16, float32, int32) -> (device, B, Hq, Hkv, N, d)
+PyObject* check_masked_attn(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 8) return PyErr_Format(PyExc_TypeError, "expected 8 arguments, got %zd", n);
+    long device = -1;
+    long long q[4], k[4], v[4], r[3], s[1];
+    int ok = whole_tensor(args[0], args[5], device, 4, q);
+    if (ok == 1) ok = whole_tensor(args[1], args[5], device, 4, k);
+    if (ok == 1) ok = whole_tensor(args[2], args[5], device, 4, v);
+    if (ok == 1) ok = k[0] == q[0] && k[2] == q[2] && k[3] == q[3] && v[0] == k[0] && v[1] == k[1] && v[2] == k[2] && v[3] == k[3];
+    if (ok != 1) return refused(ok, "Q [B, Hq, N, d], K and V [B, Hkv, N, d] must be contiguous bf16 tensors on one GPU");
+    if (args[3] != Py_None) {
+        ok = whole_tensor(args[3], args[7], device, 3, r);
+        if (ok == 1) ok = r[0] == q[0] && r[1] == q[2] && r[2] == 2;
+        if (ok != 1) return refused(ok, "ranges must be a contiguous int32 tensor [B, N, 2] on the same GPU");
+    }
+    if (args[4] != Py_None) {
+        ok = whole_tensor(args[4], args[6], device, 1, s);
+        if (ok == 1) ok = s[0] == q[1];
+        if (ok != 1) return refused(ok, kSlopes);
+    }
+    return Py_BuildValue("(lLLLLL)", device, q[0], q[1], k[1], q[2], q[3]);
+}
 // check_tensor(t, dtype, device, shape...): a contiguous tensor of that kind
 PyObject* check_tensor(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (n < 4 || n > 9) return PyErr_Format(PyExc_TypeError, "expected 4 to 9 arguments, got %zd", n);
@@ -396,9 +490,13 @@ PyMethodDef methods[] = {
     VFA_METHODS(vfa_mxfp4_quantize), VFA_METHOD(vfa_mxfp4_workspace_bytes), VFA_METHODS(vfa_mxfp4_attn_fwd), VFA_METHODS(vfa_mxfp4_attn_noexp_fwd),
     VFA_HELD_METHODS(vfa_qk_norm_rope_fwd), VFA_HELD_METHODS(vfa_kv8_append), VFA_HELD_METHODS(vfa_kv8_read), VFA_HELD_METHOD(vfa_kv8_decode_splits, 1),
     VFA_HELD_METHOD(vfa_kv8_decode_workspace_bytes, 0), VFA_HELD_METHODS(vfa_kv8_decode_fwd),
+    VFA_HELD_METHODS(vfa_kvp_append), VFA_HELD_METHOD(vfa_kvp_decode_splits, 1), VFA_HELD_METHOD(vfa_kvp_decode_workspace_bytes, 0),
+    VFA_HELD_METHODS(vfa_kvp_decode_fwd), VFA_HELD_METHODS(vfa_row_ranges), VFA_HELD_METHODS(vfa_masked_attn_fwd),
     {"check_qkv", VFA_FUNCTION(check_qkv)}, {"check_cache", VFA_FUNCTION(check_cache)},
     {"check_cache8", VFA_FUNCTION(check_cache8)}, {"check_kv8_append", VFA_FUNCTION(check_kv8_append)},
     {"check_kv8_decode", VFA_FUNCTION(check_kv8_decode)}, {"check_norm_rope", VFA_FUNCTION(check_norm_rope)}, {"check_tensor", VFA_FUNCTION(check_tensor)},
+    {"check_kvp_append", VFA_FUNCTION(check_kvp_append)}, {"check_kvp_decode", VFA_FUNCTION(check_kvp_decode)},
+    {"check_row_ranges", VFA_FUNCTION(check_row_ranges)}, {"check_masked_attn", VFA_FUNCTION(check_masked_attn)},
     {"bytes_of", &bytes_of, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "The C ABI of libvfa.so.", -1, methods, nullptr, nullptr, nullptr, nullptr};

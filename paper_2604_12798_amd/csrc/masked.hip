@@ -1,0 +1,218 @@
+// C ABI of the paged cache and of masked, capped or biased attention (declared in vfa.h): argument checks, kernel selection and launches.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+#include <math.h>
+
+#include "vfa.h"
+
+#include "common.hpp"
+#include "host.hpp"
+#include "kvp.hpp"
+#include "kvp_decode.hpp"
+#include "row_ranges.hpp"
+#include "attn_masked.hpp"
+
+namespace {
+
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+inline bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
+int launched() { return hipGetLastError() == hipSuccess ? VFA_OK : VFA_ERR_HIP; }
+
+// What the paged cache's entry points have in common; *done: there is nothing to do.
+int check_pages(const void* K, const void* V, int n_pages, const int* table, int M, int B, int Hkv, int page, int d, bool* done) {
+    *done = false;
+    if (B < 0 || Hkv <= 0 || n_pages < 0 || M < 0 || page <= 0 || d <= 0) return VFA_ERR_INVALID_ARG;
+    if ((d != 64 && d != 128) || page < 16 || (page & (page - 1)) != 0) return VFA_ERR_UNSUPPORTED;
+    if ((long long)M * page > 1LL << 30) return VFA_ERR_UNSUPPORTED;
+    if (B == 0) { *done = true; return VFA_OK; }
+    if (n_pages > 0 && (!K || !V || !aligned16(K) || !aligned16(V))) return VFA_ERR_INVALID_ARG;
+    if (M > 0 && (!table || !aligned4(table))) return VFA_ERR_INVALID_ARG;
+    if (2LL * Hkv > 65535 || (long long)B * Hkv > 65535) return VFA_ERR_UNSUPPORTED;
+    return VFA_OK;
+}
+
+int log2_of(int page) {
+    int s = 0;
+    while ((1 << s) < page) ++s;
+    return s;
+}
+
+// Strides of rows that are read 16 bytes at a time
+bool whole_runs(long long a, long long b, long long c) { return ((a | b | c) & 7) == 0; }
+
+// cap: 0 = none, else 0.001 to 1000 (see Scores)
+bool cap_ok(float cap) { return cap == 0.f || (cap >= 0.001f && cap <= 1000.f); }
+Scores scores_of(const float* slopes, float cap, float scale) { return Scores{slopes, cap * kLog2e, cap > 0.f ? 2.f * kLog2e * scale / cap : 0.f}; }
+
+template <typename F>
+void with_d(int d, F f) {
+    if (d == 128) f(std::integral_constant<int, 128>{});
+    else f(std::integral_constant<int, 64>{});
+}
+
+}  // namespace
+
+extern "C" {
+
+int vfa_kvp_append(const void* K, const void* V, void* KP, void* VP, const int* table, int B, int Hkv, int n_pages, int page, int max_pages,
+                   int n_in, int d, long long k_sb, long long k_sh, long long k_sn, long long v_sb, long long v_sh, long long v_sn,
+                   const int* old_lens, const int* new_lens, int n_old, int n_new, void* stream) {
+    bool done;
+    const int rc = check_pages(KP, VP, n_pages, table, max_pages, B, Hkv, page, d, &done);
+    if (rc != VFA_OK || n_in < 0) return rc != VFA_OK ? rc : VFA_ERR_INVALID_ARG;
+    if (!old_lens != !new_lens || !aligned4(old_lens) || !aligned4(new_lens)) return VFA_ERR_INVALID_ARG;
+    const int cap = max_pages * page;
+    if (!old_lens && (n_old < 0 || n_old > n_new || n_new > cap || n_new - n_old > n_in)) return VFA_ERR_INVALID_ARG;
+    if (done || cap == 0 || n_pages == 0 || n_in == 0 || (!old_lens && n_old == n_new)) return VFA_OK;
+    if (!K || !V || !aligned16(K) || !aligned16(V) || !whole_runs(k_sb, k_sh, k_sn) || !whole_runs(v_sb, v_sh, v_sn)) return VFA_ERR_INVALID_ARG;
+    KvpAppend p{};
+    p.X[0] = (const uint16_t*)K; p.X[1] = (const uint16_t*)V;
+    p.sb[0] = k_sb; p.sh[0] = k_sh; p.sn[0] = k_sn;
+    p.sb[1] = v_sb; p.sh[1] = v_sh; p.sn[1] = v_sn;
+    p.Y[0] = (uint16_t*)KP; p.Y[1] = (uint16_t*)VP;
+    p.table = table; p.old_lens = old_lens; p.new_lens = new_lens; p.old_len = n_old; p.new_len = n_new;
+    p.n_in = n_in; p.n_pages = n_pages; p.M = max_pages; p.Hkv = Hkv; p.sh_page = log2_of(page);
+    hipStream_t s = (hipStream_t)stream;
+    (void)hipGetLastError();
+    const int rows = 2 * B * Hkv;
+    if (n_in == 1) {
+        with_d(d, [&](auto d_c) { kvp_append_kernel<decltype(d_c)::value, true><<<(unsigned)ceil_div(rows, 512 / d), 64, 0, s>>>(p, rows); });
+        return launched();
+    }
+    const int most = min(n_in, cap), each = 4 * 2048 / d;
+    const long long groups = ((long long)(old_lens ? most : n_new - n_old) + each - 1) / each;
+    if (groups * 2 * Hkv * B > kMaxWorkgroups256) return VFA_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)groups, (unsigned)(2 * Hkv), (unsigned)B);
+    with_d(d, [&](auto d_c) { kvp_append_kernel<decltype(d_c)::value, false><<<grid, 256, 0, s>>>(p, rows); });
+    return launched();
+}
+
+int vfa_kvp_decode_splits(int B, int Hq, int Hkv, int n_q, int d, int n_keys, int varlen) {
+    if (B <= 0 || Hq <= 0 || Hkv <= 0 || n_q <= 0 || n_keys <= 0 || (long long)B * Hkv > 65535) return 1;
+    const int n_cu = cu_count() > 0 ? cu_count() : 256, all = n_keys / BN + (n_keys % BN != 0);  // (n_keys + 63 may not fit)
+    const long long rows = (long long)(Hq / Hkv) * n_q;
+    const int g = Hq / Hkv, tokens = rows <= 32 ? n_q : g < 32 ? 32 / g : 1;
+    const long long heads = (long long)B * Hkv * (((long long)n_q + tokens - 1) / tokens);  // (with more than 32 rows, groups of them)
+    if (all <= 8) return 1;
+    const long long n = varlen && B > 1 ? (2LL * n_cu + heads - 1) / heads : n_cu / heads;
+    return (int)max(1LL, min(n, (all + 3) / 4LL));
+}
+
+size_t vfa_kvp_decode_workspace_bytes(int B, int Hq, int n_q, int d, int n_splits) {
+    if (B <= 0 || Hq <= 0 || n_q <= 0 || d <= 0 || n_splits <= 0) return 0;
+    const size_t bytes = (size_t)B * Hq * n_q * n_splits * (2 + (size_t)d) * sizeof(float) + 2 * sizeof(int) * (size_t)B;
+    return (bytes + 255) & ~(size_t)255;
+}
+
+int vfa_kvp_decode_fwd(const void* Q, const void* KP, const void* VP, const int* table, void* O, float* LSE, int B, int Hq, int Hkv, int n_pages,
+                       int page, int max_pages, int n_q, int d, const int* seq_lens, int n_keys, int n_splits, float softmax_scale,
+                       float score_cap, const float* slopes, void* workspace, size_t workspace_bytes, void* stream) {
+    bool done;
+    const int rc = check_pages(KP, VP, n_pages, table, max_pages, B, Hkv, page, d, &done);
+    if (rc != VFA_OK) return rc;
+    const int n_cap = max_pages * page;
+    if (Hq <= 0 || Hq % Hkv != 0 || n_q < 0 || n_splits < 1 || n_splits > 4096 || !isfinite(softmax_scale) || !cap_ok(score_cap)) return VFA_ERR_INVALID_ARG;
+    if (!aligned4(seq_lens) || !aligned4(slopes) || (!seq_lens && (n_keys < 0 || n_keys > n_cap))) return VFA_ERR_INVALID_ARG;
+    const int g = Hq / Hkv;
+    if (g > 32) return VFA_ERR_UNSUPPORTED;
+    const long long rows = (long long)g * n_q;
+    if (done || n_q == 0) return VFA_OK;
+    if (!Q || !O || !aligned16(Q) || !aligned16(O) || !aligned4(LSE)) return VFA_ERR_INVALID_ARG;
+    const bool grouped = rows > 32;
+    const int tokens = grouped ? 32 / g : n_q;
+    const long long groups = ((long long)n_q + tokens - 1) / tokens, out_rows = (long long)B * Hq * n_q;
+    if (grouped && groups * n_splits > 65535) return VFA_ERR_UNSUPPORTED;
+    const long long wgs = (long long)B * Hkv * n_splits * groups;
+    if (out_rows > 0x7fffffffLL || wgs > kMaxWorkgroups256 / 2 || (n_splits > 1 && out_rows > kMaxWorkgroups256)) return VFA_ERR_UNSUPPORTED;
+    if (n_splits > 1 && (!workspace || !aligned16(workspace) || workspace_bytes < vfa_kvp_decode_workspace_bytes(B, Hq, n_q, d, n_splits)))
+        return VFA_ERR_INVALID_ARG;
+    if (n_cap == 0) n_splits = 1;  // (no keys, so no ranges to deal out)
+    KvpDecode P{};
+    DecodeParams& p = P.d;
+    P.table = table; P.n_pages = n_pages; P.M = max_pages; P.sh_page = log2_of(page); P.n_q = n_q; P.g = g; P.tokens = tokens; P.groups = (int)groups;
+    p.Q = (const uint16_t*)Q; p.K = (const uint16_t*)KP; p.V = (const uint16_t*)VP; p.O = (uint16_t*)O; p.LSE = LSE;
+    p.B = B; p.Hq = Hq * n_q; p.Hkv = Hkv; p.n_cap = n_cap; p.n_keys = seq_lens ? n_cap : n_keys; p.seq_lens = seq_lens; p.n_splits = n_splits;
+    p.g = (int)rows;
+    const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)d);
+    p.c = scale * kLog2e;
+    P.s = scores_of(slopes, score_cap, scale);
+    const size_t slots = (size_t)B * Hq * n_q * n_splits;
+    p.opart = (float*)workspace; p.pm = p.opart + slots * d; p.lpart = p.pm + slots; p.dealt = (int*)(p.lpart + slots);
+    hipStream_t s = (hipStream_t)stream;
+    const int n_cu = cu_count() > 0 ? cu_count() : 256;
+    (void)hipGetLastError();
+    const bool dealt = seq_lens && n_splits > 1 && B > 1 && (B <= 64 || (B <= DEAL_MAX_B && (long long)B * Hkv * n_splits <= 8LL * n_cu && ceil_div(n_cap, BN) > 2 * n_splits));
+    with_d(d, [&](auto d_c) {
+        constexpr int D = decltype(d_c)::value;
+        auto launch = [&](auto halves_c) {
+            constexpr bool HALVES = decltype(halves_c)::value;
+            const dim3 grid((unsigned)n_splits, (unsigned)B, (unsigned)Hkv);
+            if (!seq_lens) kvp_decode_kernel<D, 4, LENS_ONE, false, HALVES><<<grid, 256, 0, s>>>(P);
+            else if (dealt) kvp_decode_kernel<D, 4, LENS_DEALT, false, HALVES><<<grid, 256, 0, s>>>(P);
+            else kvp_decode_kernel<D, 4, LENS_FIXED, false, HALVES><<<dim3((unsigned)n_splits, (unsigned)Hkv, (unsigned)B), 256, 0, s>>>(P);
+        };
+        if (grouped) {
+            const dim3 grid((unsigned)Hkv, (unsigned)(groups * n_splits), (unsigned)B);
+            if (!seq_lens) kvp_decode_kernel<D, 4, LENS_ONE, true, false><<<grid, 256, 0, s>>>(P);
+            else if (dealt) kvp_decode_kernel<D, 4, LENS_DEALT, true, false><<<grid, 256, 0, s>>>(P);
+            else kvp_decode_kernel<D, 4, LENS_FIXED, true, false><<<grid, 256, 0, s>>>(P);
+        } else if (rows <= 16) {
+            launch(std::true_type{});
+        } else {
+            launch(std::false_type{});
+        }
+        if (n_splits == 1) return;
+        const dim3 grid((unsigned)p.Hq, (unsigned)B);
+        if (dealt) decode_merge_kernel<D, SLOTS_TABLE, true><<<grid, 256, 0, s>>>(p);
+        else decode_merge_kernel<D, SLOTS_FIXED, true><<<grid, 256, 0, s>>>(p);
+    });
+    return launched();
+}
+
+int vfa_row_ranges(const int* doc_offsets, const int* prefix_lens, int* ranges, int B, int N, int n_docs, int causal, void* stream) {
+    if (B < 0 || N < 0 || n_docs < 0 || (causal != 0 && causal != 1)) return VFA_ERR_INVALID_ARG;
+    if (!aligned4(doc_offsets) || !aligned4(prefix_lens) || !aligned8(ranges)) return VFA_ERR_INVALID_ARG;
+    if (B == 0 || N == 0) return VFA_OK;
+    if (!doc_offsets || !ranges) return VFA_ERR_INVALID_ARG;
+    const long long groups = ((long long)N + 255) / 256;
+    if (B > 65535 || n_docs == 0x7fffffff || groups * B > kMaxWorkgroups256) return VFA_ERR_UNSUPPORTED;
+    const RowRanges p{doc_offsets, prefix_lens, reinterpret_cast<int2*>(ranges), N, n_docs, causal};
+    (void)hipGetLastError();
+    row_ranges_kernel<<<dim3((unsigned)groups, (unsigned)B), 256, 0, (hipStream_t)stream>>>(p);
+    return launched();
+}
+
+int vfa_masked_attn_fwd(const void* Q, const void* K, const void* V, void* O, float* LSE, int B, int Hq, int Hkv, int N, int d, int causal,
+                        const int* ranges, float softmax_scale, float score_cap, const float* slopes, void* stream) {
+    if (B < 0 || Hq <= 0 || Hkv <= 0 || N < 0 || d <= 0 || Hq % Hkv != 0 || (causal != 0 && causal != 1)) return VFA_ERR_INVALID_ARG;
+    if (!isfinite(softmax_scale) || !cap_ok(score_cap)) return VFA_ERR_INVALID_ARG;
+    if (d != 64 && d != 128) return VFA_ERR_UNSUPPORTED;
+    if (!aligned8(ranges) || !aligned4(slopes) || !aligned4(LSE)) return VFA_ERR_INVALID_ARG;
+    if (B == 0 || N == 0) return VFA_OK;
+    if (!Q || !K || !V || !O || !aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O)) return VFA_ERR_INVALID_ARG;
+    const long long blocks = ((long long)N + 127) / 128, heads = (long long)B * Hq;
+    if ((long long)N * 2 * d > 0x7fffffffLL || heads > 0x7fffffffLL / blocks || heads * blocks > kMaxWorkgroups256) return VFA_ERR_UNSUPPORTED;
+    MaskedParams P{};
+    Params& p = P.a;
+    p.Q = (const uint16_t*)Q; p.K = (const uint16_t*)K; p.V = (const uint16_t*)V; p.O = (uint16_t*)O; p.LSE = LSE;
+    p.B = B; p.Hq = Hq; p.Hkv = Hkv; p.N = N; p.Tr = (int)blocks; p.Tc = ceil_div(N, BN); p.causal = causal;
+    set_items(p, false);
+    const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)d);
+    p.c = scale * kLog2e;
+    P.s = scores_of(slopes, score_cap, scale);
+    P.ranges = reinterpret_cast<const int2*>(ranges);
+    P.unit = 1.f / scale;
+    const unsigned grid = (unsigned)(heads * blocks);
+    (void)hipGetLastError();
+    with_d(d, [&](auto d_c) {
+        constexpr int D = decltype(d_c)::value;
+        hipStream_t s = (hipStream_t)stream;
+        if (score_cap > 0.f && slopes) attn_masked_kernel<D, true, true><<<grid, 256, 0, s>>>(P);
+        else if (score_cap > 0.f) attn_masked_kernel<D, true, false><<<grid, 256, 0, s>>>(P);
+        else if (slopes) attn_masked_kernel<D, false, true><<<grid, 256, 0, s>>>(P);
+        else attn_masked_kernel<D, false, false><<<grid, 256, 0, s>>>(P);
+    });
+    return launched();
+}
+
+}  // extern "C"
