@@ -6,14 +6,24 @@
 namespace {
 
 // ---------------------------------------------------------------------------------------------
-// Row i sees the keys [lo, hi) of its entry in `ranges` (all without one), and with `causal` none behind itself.  A workgroup of four waves has 128
-// rows of a head, a wave 32 of them; it goes over the tiles from the first key that any of its rows sees to the last, and a wave leaves out those that none of
-// its own rows sees.  Exact running max.
+// Row i sees the keys [lo, hi) of its entry in `ranges` (all without one), and with `causal` none behind itself.  A workgroup has 32 RW rows of a head and
+// goes over the steps of 32 KQ keys from the first key that any of its rows sees to the last; wave (rw, kq) multiplies the 32 keys of group kq with
+// rows 32 rw .. 32 rw + 31, and leaves out the steps at either end that none of its own rows sees.
+//
+// A score's log2 weight is A + F v.  Without a cap v is what the matrix unit gives and F = c; with one v = 1 / (1 + e^(2 s / cap)), F = -2 cap2 and A = cap2 (see
+// Scores).  A bias -slope |i - j| is linear in the key's place in the step on either side of the row: that part goes into v, one multiply-add with a
+// constant, and the rest is the step's A.
+//
+// Iteration s of a wave: Q.K^T of its step s + 1 and P.V of its step s - 1, a product of each in turn, with the softmax of step s dealt out between them.  (The two
+// waves of a SIMD do not fill each other's gaps: one after the other a tile's products and its vector work took their sum.)  Its max is a reference,
+// the row's max plus kMaskedKeep when it last moved, which moves only when a score passes it.
+// Steps that a wave sees in part, the first and last ones, take the same three parts one after the other.
+constexpr float kMaskedKeep = 8.f;
+
 struct MaskedParams {
     Params a;          // Q, K, V, O, LSE, sizes, items, c
     Scores s;
     const int2* ranges;
-    float unit;        // 1 / scale: a bias in units of raw scores
 };
 
 template <typename F>
@@ -28,21 +38,41 @@ __device__ __forceinline__ int wave_fold(int x, F f) {
     return __builtin_amdgcn_readfirstlane(f((int)b[0], (int)b[1]));
 }
 
-template <int D, bool CAP, bool BIAS>
+__device__ __forceinline__ void request1_at(const u32x4& rsrc, uint32_t at, uint32_t o0, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 :
+                 : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(o0), "s"(rsrc), "s"(__builtin_amdgcn_readfirstlane(at))
+                 : "memory", "m0");
+}
+
+template <int D, int RW, int KQ>
+struct Masked {
+    static constexpr int KT = 32 * KQ;                 // keys of a step
+    static constexpr int SLOT = KT * Tile<D>::ROWB;    // of K or V
+    static constexpr int S = KQ == 1 ? 4 : 2;          // slots of each
+    static constexpr int LI = SLOT / 4096;             // load instructions of a wave and slot
+    static constexpr bool AHEAD = S == 4;              // slots are there a step early, and a step's first fragments are read in the one before
+    static constexpr int R = !AHEAD ? 3 : D == 128 ? 8 : 4;  // fragments under way
+    static constexpr int LDS_BYTES = 2 * S * SLOT;
+    static_assert(RW * KQ == 4, "four waves");
+    static_assert(KQ == 1 || 4 * (D * 64 + 256) <= LDS_BYTES, "the partial sums have to fit the slots' memory");
+};
+
+template <int D, int RW, int KQ, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams P) {
     const Params& p = P.a;
     using T = Tile<D>;
-    constexpr int NW = 4, BM = 32 * NW, KK = D / 16, DB = D / 32;
-    constexpr int LI = T::BYTES / 1024 / NW, RPI = 1024 / T::ROWB;
-    __shared__ __attribute__((aligned(16))) uint8_t smem[4 * T::BYTES];  // K[2], V[2]
-    __shared__ uint64_t bad[NW];  // keys of the tile with values that are not finite, by the wave that found them
-    uint8_t* const Ks = smem;
-    uint8_t* const Vs = smem + 2 * T::BYTES;
+    using F = Masked<D, RW, KQ>;
+    constexpr int BM = 32 * RW, KK = D / 16, DB = D / 32, KT = F::KT, S = F::S, LI = F::LI, RPI = 1024 / T::ROWB;
+    __shared__ __attribute__((aligned(16))) uint8_t smem[F::LDS_BYTES];  // K[S], V[S]
+    __shared__ uint64_t bad[4];  // keys of a slot with values that are not finite, by the wave that found them
+    uint8_t* const Vs = smem + S * F::SLOT;
     const int tid = threadIdx.x, lane = tid & 63, ql = lane & 31, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int rw = wave % RW, kq = wave / RW;
     const auto [head, kv, i] = item_of(p, blockIdx.x);
     const int N = p.N, row0 = i * BM, b = kv / p.Hkv;
-    const int qrow = row0 + 32 * wave + ql, qrow_c = min(qrow, N - 1);
+    const int qrow0 = row0 + 32 * rw, qrow = qrow0 + ql, qrow_c = min(qrow, N - 1);
     // the keys [x, y) that a row sees; one that sees none has [0, 0)
     auto range_of = [&](int r) {
         int2 k = {0, N};
@@ -56,105 +86,332 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
     };
     const auto lesser = [](int x, int y) { return min(x, y); };
     const auto larger = [](int x, int y) { return max(x, y); };
-    const int2 own = range_of(qrow_c);
     const int far = 0x7fffffff;
-    // of the wave: the first and the last key that any row sees, and what all rows see
-    const int any_lo = wave_fold(own.x < own.y ? own.x : far, lesser), any_hi = wave_fold(own.y, larger);
-    const int all_lo = wave_fold(own.x, larger), all_hi = wave_fold(own.y, lesser);
-    // of the workgroup
-    int wg_lo, wg_hi, wg_all_lo, wg_all_hi;
+    // of the wave: the first and the last key that any row sees, and what all rows see; of the workgroup
+    int2 own;
+    int any_lo, any_hi, all_lo, all_hi, wg_lo, wg_hi, wg_all_lo, wg_all_hi;
     {
-        const int2 r0 = range_of(min(row0 + lane, N - 1)), r1 = range_of(min(row0 + 64 + lane, N - 1));
+        own = range_of(qrow_c);
+        const int2 r0 = range_of(min(row0 + lane, N - 1)), r1 = BM == 128 ? range_of(min(row0 + 64 + lane, N - 1)) : r0;
+        any_lo = wave_fold(own.x < own.y ? own.x : far, lesser);
+        any_hi = wave_fold(own.y, larger);
+        all_lo = wave_fold(own.x, larger);
+        all_hi = wave_fold(own.y, lesser);
         wg_lo = wave_fold(min(r0.x < r0.y ? r0.x : far, r1.x < r1.y ? r1.x : far), lesser);
         wg_hi = wave_fold(max(r0.y, r1.y), larger);
         wg_all_lo = wave_fold(max(r0.x, r1.x), larger);
         wg_all_hi = wave_fold(min(r0.y, r1.y), lesser);
     }
-    // ---- requests: a wave moves LI adjacent pieces (1 KiB of whole rows) of a tile, by buffer loads whose buffer is the head's keys: rows past the end
-    // of the sequence are out of its range and LDS gets zeros
+    const int s_lo = wg_lo < wg_hi ? wg_lo / KT : 0, s_hi = wg_lo < wg_hi ? (wg_hi + KT - 1) / KT : 0;
+    // steps of the wave: [o_lo, o_hi)
+    const int o_lo = any_lo < any_hi ? max((any_lo - 32 * kq - 31 + KT - 1) / KT, s_lo) : s_hi, o_hi = any_hi > 32 * kq ? (any_hi - 32 * kq + KT - 1) / KT : 0;
+
+    // ---- requests: a wave moves LI adjacent pieces (1 KiB of whole rows) of a slot, by buffer loads whose buffer is the head's keys: rows past the end
+    // of the sequence are out of its range and LDS gets zeros, as for steps before the first one and past the last
     const int r_own = RPI * LI * wave + lane / T::CH, cp = lane % T::CH;
     uint32_t offK[LI];
 #pragma unroll
     for (int u = 0; u < LI; ++u) offK[u] = (uint32_t)(r_own * T::ROWB + ((cp ^ T::k_mix(r_own + RPI * u)) << 4));
     const uint32_t offV = (uint32_t)(r_own * T::ROWB + ((cp ^ T::v_mix(r_own)) << 4));  // (the same for all pieces)
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(smem) + wave * LI * 1024);
-    const uint32_t bytes = (uint32_t)N * T::ROWB;  // (launched for fewer than 2^32)
+    const uint32_t bytes = (uint32_t)N * T::ROWB;  // (launched for fewer than 2^31)
     const u32x4 rsrcK = tile_buffer((uint64_t)(uintptr_t)(p.K + (size_t)kv * N * D), bytes), rsrcV = tile_buffer((uint64_t)(uintptr_t)(p.V + (size_t)kv * N * D), bytes);
-    auto request = [&](int t, int buf) __attribute__((always_inline)) {
-        const uint32_t at = (uint32_t)t * T::BYTES;
-        if constexpr (LI == 4) {
-            request4_at(rsrcK, at, offK[0], offK[1], offK[2], offK[3], lds0 + buf * T::BYTES);
-            request4_at(rsrcV, at, offV, offV, offV, offV, lds0 + (2 + buf) * T::BYTES);
-        } else {
-            request2_at(rsrcK, at, offK[0], offK[1], lds0 + buf * T::BYTES);
-            request2_at(rsrcV, at, offV, offV, lds0 + (2 + buf) * T::BYTES);
-        }
+    auto request = [&](const u32x4& rsrc, int s, int slot, bool is_v) __attribute__((always_inline)) {
+        const uint32_t at = s >= s_lo && s < s_hi ? (uint32_t)s * F::SLOT : bytes, to = lds0 + slot * F::SLOT;
+        if constexpr (LI == 4) request4_at(rsrc, at, is_v ? offV : offK[0], is_v ? offV : offK[1], is_v ? offV : offK[2], is_v ? offV : offK[3], to);
+        else if constexpr (LI == 2) request2_at(rsrc, at, is_v ? offV : offK[0], is_v ? offV : offK[1], to);
+        else request1_at(rsrc, at, is_v ? offV : offK[0], to);
     };
-    const int t_lo = wg_lo / BN, t_hi = wg_lo < wg_hi ? (wg_hi + BN - 1) / BN : t_lo;
-    if (t_lo < t_hi) request(t_lo, 0);
     bf16x8 qf[KK];
-    {
-        const uint16_t* const Qg = p.Q + ((size_t)head * N + qrow_c) * D;
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(Qg + 16 * kk + 8 * hh);
-    }
-    const float slope2 = BIAS ? P.s.slopes[head % p.Hq] * kLog2e : 0.f;
     f32x16 ot[DB];
 #pragma unroll
     for (int db = 0; db < DB; ++db) ot[db] = f32x16{0};
     float m2 = -INFINITY, lsum = 0.f;
-    const float c = CAP || BIAS ? 1.f : p.c;
-    // (one body with a branch around the mask: two bodies were given accumulators of their own, and spilled)
-    auto tile = [&](int t, int buf, bool masked) __attribute__((always_inline)) {
-        f32x16 st[2];
-        uint32_t pk[16];
-        __builtin_amdgcn_s_setprio(1);
-        qk_tile_pipe<D>(Ks + buf * T::BYTES, qf, st, ql, hh);
-        __builtin_amdgcn_s_setprio(0);
-        const int key0 = t * BN + 4 * hh;
-        if (CAP) cap_scores(P.s, st);
-        if (BIAS) bias_scores(P.s, p.c, st, slope2, (float)(qrow - key0));
-        if (masked) {
-            const uint32_t first = own.x - key0, many = own.y - own.x;
+
+    if (s_lo < s_hi) {  // (the same in all waves)
+        // slot of step s: (s - s_lo) mod S.  The first iteration takes the last slot of V for that of the step before it: zeros
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-                const uint32_t k = 32 * (e >> 4) + 8 * ((e & 15) >> 2) + (e & 3);
-                const bool ok = k - first < many;
-                st[e >> 4][e & 15] = ok ? st[e >> 4][e & 15] : -INFINITY;
+        for (int e = 0; e < S - 1; ++e) request(rsrcK, s_lo + e, e, false);
+#pragma unroll
+        for (int e = 0; e < S - 3; ++e) request(rsrcV, s_lo + e, S + e, true);
+#pragma unroll
+        for (int u = 0; u < LI; ++u) *reinterpret_cast<u32x4*>(Vs + (S - 1) * F::SLOT + (wave * LI + u) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+        {
+            const uint16_t* const Qg = p.Q + ((size_t)head * N + qrow_c) * D;
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(Qg + 16 * kk + 8 * hh);
+        }
+        const float slope2 = BIAS ? P.s.slopes[head % p.Hq] * kLog2e : 0.f;
+        const float fac = CAP ? -2.f * P.s.cap2 : p.c;
+        const float lin = BIAS ? slope2 / fac : 0.f;  // the bias of a key's distance, in units of v
+        wait_vm0_and_sync();
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(qf[kk]));  // (waited for here, not in the steps)
+
+        uint32_t ka[KK], va[DB];
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) ka[kk] = lds_addr(smem) + (T::k_base(ql, hh) ^ (kk << 5)) + 32 * kq * T::ROWB;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) va[db] = lds_addr(Vs) + (T::v_base(lane, hh) ^ (db << 6)) + 32 * kq * T::ROWB;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(ka[kk]));  // (sums of a scalar and a vector that the compiler would add up again for each load)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) asm volatile("" : "+v"(va[db]));
+        auto ld_k = [&](uint32_t slot, int kk) __attribute__((always_inline)) { return *(lds_frag)(ka[kk] + slot); };
+        auto ld_v = [&](uint32_t slot, int f) __attribute__((always_inline)) {
+            const uint32_t a = va[f % DB] + (slot + 16 * (f / DB) * T::ROWB);
+            const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(a));
+            const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(a + 8 * T::ROWB));
+            const u32x2 a0 = __builtin_bit_cast(u32x2, v0), a1 = __builtin_bit_cast(u32x2, v1);
+            return __builtin_bit_cast(bf16x8, u32x4{a0[0], a0[1], a1[0], a1[1]});
+        };
+        auto pf = [&](const uint32_t* pk, int c) __attribute__((always_inline)) {
+            return __builtin_bit_cast(bf16x8, u32x4{pk[4 * c], pk[4 * c + 1], pk[4 * c + 2], pk[4 * c + 3]});
+        };
+        // (all in steps, worked out once) Sides of a bias: the wave's keys of step s all at or before all of its rows; all at or behind all of them.
+        // Steps that all rows of the wave see whole, and all rows of the workgroup
+        const int l_hi = qrow0 >= 32 * kq + 31 ? (qrow0 - 32 * kq - 31) / KT + 1 : 0, r_lo = (max(qrow0 + 31 - 32 * kq, 0) + KT - 1) / KT;
+        const int w_lo = (max(all_lo - 32 * kq, 0) + KT - 1) / KT, w_hi = all_hi >= 32 * kq + 32 ? (all_hi - 32 * kq - 32) / KT + 1 : 0;
+        const int f_lo = (wg_all_lo + KT - 1) / KT, f_hi = wg_all_hi / KT;
+        auto left = [&](int s) { return !BIAS || s < l_hi; };
+        auto right = [&](int s) { return s >= r_lo; };
+        auto whole = [&](int s) { return s >= w_lo && s < w_hi; };
+
+        // the softmax of a step, in parts: pairs of scores to v (CAP), the max, pairs of v to weights
+        float add, alpha;   // A - the max; what the sums so far are to be multiplied with
+        bool moved;         // (of the wave)
+        auto offset = [&](int s) __attribute__((always_inline)) {  // A
+            const int away = qrow - s * KT - 32 * kq - 4 * hh;
+            const float base = BIAS ? slope2 * (float)(left(s) ? -away : away) : 0.f;
+            return CAP ? P.s.cap2 + base : base;
+        };
+        auto part_a = [&](f32x16& st, int s, int q) __attribute__((always_inline)) {
+#pragma unroll
+            for (int e = 2 * q; e < 2 * q + 2; ++e) {
+                if (CAP) st[e] = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(st[e] * P.s.capk));
+                if (BIAS) st[e] = __builtin_fmaf(left(s) ? lin : -lin, (float)(8 * (e >> 2) + (e & 3)), st[e]);
             }
-        }
-        softmax_tile<true, false, DB, true, true>(st, pk, ot, m2, lsum, c, 0, 0, hh, 0.f);
-        __builtin_amdgcn_s_setprio(1);
-        pv_tile_pipe<D>(Vs + buf * T::BYTES, pk, ot, lane, hh);
-        __builtin_amdgcn_s_setprio(0);
-    };
-    wait_vm0_and_sync();
-    for (int t = t_lo; t < t_hi; ++t) {
-        const int buf = (t - t_lo) & 1, k0 = t * BN;
-        if (t + 1 < t_hi) request(t + 1, buf ^ 1);
-        // (no row of the workgroup may get what is not finite among the values of a key that it does not see)
-        const bool part = !(k0 >= wg_all_lo && k0 + BN <= wg_all_hi);
-        if (part) {
-            bad[wave] = clear_not_finite<D, LI>(Vs + buf * T::BYTES, wave * LI, lane);
-            __syncthreads();
-        }
-        if (k0 < any_hi && k0 + BN > any_lo) {
-            tile(t, buf, !(k0 >= all_lo && k0 + BN <= all_hi));
-        }
-        if (part) {
-            uint64_t keys = bad[0] | bad[1] | bad[2] | bad[3];
+        };
+        auto part_m = [&](const f32x16& st, int s) __attribute__((always_inline)) {
+            float x = st[0];
+#pragma unroll
+            for (int q = 0; q < 7; ++q) x = CAP ? fminf(fminf(x, st[1 + 2 * q]), st[2 + 2 * q]) : fmaxf(fmaxf(x, st[1 + 2 * q]), st[2 + 2 * q]);
+            x = CAP ? fminf(x, st[15]) : fmaxf(x, st[15]);
+            const float a = offset(s), y = __builtin_fmaf(x, fac, a);  // (A differs between the halves)
+            const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
+            const float top = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
+            const bool up = top > m2;  // (each row by itself: what the others see changes none of its bits)
+            moved = __builtin_amdgcn_ballot_w64(up) != 0;
+            const float m_new = up ? top + kMaskedKeep : m2, msub = finite_max(m_new);
+            alpha = __builtin_amdgcn_exp2f(m2 - msub);
+            lsum *= alpha;
+            m2 = m_new;
+            add = a - msub;
+        };
+        auto part_b = [&](const f32x16& st, uint32_t* pk, int q) __attribute__((always_inline)) {
+            const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(st[2 * q], fac, add)), e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(st[2 * q + 1], fac, add));
+            lsum += e0;
+            lsum += e1;
+            pk[q] = pack_bf16(e0, e1);
+            asm volatile("" : "+v"(pk[q]), "+v"(lsum));  // (here, between the products: the compiler sank them behind the next branch)
+        };
+        auto rescale = [&]() __attribute__((always_inline)) {
+            if (moved) {
+#pragma unroll
+                for (int db = 0; db < DB; ++db) ot[db] *= alpha;
+            }
+        };
+        constexpr int R = F::R;
+        static_assert(!F::AHEAD || 2 * KK % R == 0, "a step ends where the ring of fragments began");
+        bf16x8 fr[R];
+        // Iteration s: st, pk of step s; sn of step s + 1, po of step s - 1
+        auto work = [&](int s, f32x16& st, f32x16& sn, uint32_t* pk, const uint32_t* po, uint32_t slot_k, uint32_t slot_v, uint32_t next_k, uint32_t next_v) __attribute__((always_inline)) {
+            constexpr bool A = CAP || BIAS;
+            constexpr int M = 2 * KK, H = A ? M / 2 : 0;  // products; those in front of the masks
+            static_assert(KK == 2 * DB, "as many products on either side");
+            auto frag = [&](int e, uint32_t sk, uint32_t sv) __attribute__((always_inline)) { return e & 1 ? ld_v(sv, e >> 1) : ld_k(sk, e >> 1); };
+            auto product = [&](int e) __attribute__((always_inline)) {
+                if (e & 1) {
+                    const int f = e >> 1;
+                    ot[f % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[e % R], pf(po, f / DB), ot[f % DB], 0, 0, 0);
+                } else {
+                    sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[e % R], qf[e >> 1], e == 0 ? f32x16{0} : sn, 0, 0, 0);
+                }
+                if (e + R < M) fr[e % R] = frag(e + R, slot_k, slot_v);
+                else if (F::AHEAD) fr[e % R] = frag(e + R - M, next_k, next_v);
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            if (!F::AHEAD) {
+#pragma unroll
+                for (int e = 0; e < R; ++e) fr[e] = frag(e, slot_k, slot_v);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int e = 0; e < H; ++e) {
+#pragma unroll
+                for (int u = 8 * e / H; u < 8 * (e + 1) / H; ++u) part_a(st, s, u);
+                product(e);
+            }
+            const int key0 = s * KT + 32 * kq + 4 * hh;
+            if (BIAS && !left(s) && !right(s)) {  // (part_a counts the distance as if on the right)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) st[r] = __builtin_fmaf(-2.f * lin, fmaxf((float)(qrow - key0 - 8 * (r >> 2) - (r & 3)), 0.f), st[r]);
+            }
+            if (!whole(s)) {
+                const uint32_t first = own.x - key0, many = own.y - own.x;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) st[r] = (uint32_t)(8 * (r >> 2) + (r & 3)) - first < many ? st[r] : CAP ? INFINITY : -INFINITY;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int e = H; e < M; ++e) {
+#pragma unroll
+                for (int u = 10 * (e - H) / (M - H); u < 10 * (e - H + 1) / (M - H); ++u) {
+                    if (u == 0) part_m(st, s);
+                    else if (u >= 2) part_b(st, pk, u - 2);
+                }
+                product(e);
+            }
+            rescale();
+        };
+        // What surrounds the work of an iteration; j = s - s_lo (mod S)
+        uint64_t keys = 0;  // of the step whose values are multiplied: those with values that are not finite
+        auto iteration = [&](int s, int j, auto f) __attribute__((always_inline)) {
+            const uint32_t slot_v = (j + S - 1) % S * F::SLOT;
+            // No row of the workgroup may get what is not finite among the values of a key that it does not see: those of a step that not all rows see whole
+            // are cleared before the first of them is read
+            const int c = F::AHEAD ? s : s - 1;
+            uint64_t found = 0;
+            if (c >= s_lo && c < s_hi && !(c >= f_lo && c < f_hi)) {
+                bad[wave] = clear_not_finite<D, LI>(Vs + (F::AHEAD ? j * F::SLOT : slot_v), wave * LI, lane);
+                __syncthreads();
+                found = bad[0] | bad[1] | bad[2] | bad[3];
+                found = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(found >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)found);
+            }
+            if (!F::AHEAD) keys = found;
+            request(rsrcK, s + S, j % S, false);
+            request(rsrcV, s - 2 + S, S + (j + S - 2) % S, true);
+            f((j + 1) % S * F::SLOT, slot_v);
             if (__builtin_expect(keys != 0, 0)) {
                 const uint16_t* const Vg = p.V + (size_t)kv * N * D;
+                // (the max may have moved behind the product: what is added is not finite, whatever it is multiplied with)
 #pragma unroll 1
-                for (; keys; keys &= keys - 1) {
-                    const int k = k0 + __builtin_ctzll(keys);  // (a key of the sequence: behind its end LDS has zeros)
+                for (uint64_t left_over = keys >> (32 * kq) & 0xffffffffull; left_over; left_over &= left_over - 1) {
+                    const int k = (s - 1) * KT + 32 * kq + __builtin_ctzll(left_over);  // (a key of the sequence: behind its end LDS has zeros)
                     add_not_finite<D>(Vg + (size_t)k * D, k >= own.x && k < own.y, ot, hh);
                 }
             }
+            keys = found;
+            // K of step s + 2 and V of step s are there, AHEAD those of the steps behind them; reads of slots that are written next are through with their products
+            __builtin_amdgcn_s_waitcnt(F::AHEAD ? 0x0F70 | 2 * LI : 0x0070);
+            __builtin_amdgcn_s_barrier();
+        };
+        // Iterations [front, o_hi] are the wave's (the slots are constants, so the first one is the first of a round); its scores of step `front` come from the
+        // one before.  What is not the wave's among their steps is masked, so its weights are 0, and the values that they meet are finite: cleared, or,
+        // in the first iteration of all, the slot of zeros.
+        const bool any = o_lo < o_hi;
+        const int front = any ? s_lo + (o_lo - s_lo) / S * S : s_hi + 2;
+        int s = s_lo - 1, j = S - 1;
+        auto idle = [&](int end) __attribute__((always_inline)) {
+            for (; s < end; ++s) {
+                iteration(s, j, [](uint32_t, uint32_t) {});
+                j = j + 1 == S ? 0 : j + 1;
+            }
+        };
+        idle(min(front - 1, s_hi + 1));
+        if (any) {
+            f32x16 sa, sb;
+            uint32_t pa[8], pb[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) pa[q] = 0;
+            iteration(s, S - 1, [&](uint32_t, uint32_t) __attribute__((always_inline)) {
+                sa = f32x16{0};
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk) sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_k(0, kk), qf[kk], sa, 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+                if (F::AHEAD) {  // (of K of step front + 1, V of step front - 1)
+#pragma unroll
+                    for (int e = 0; e < R; ++e) fr[e] = e & 1 ? ld_v((S - 1) * F::SLOT, e >> 1) : ld_k(F::SLOT, e >> 1);
+                }
+            });
+            ++s;
+            for (;;) {
+                auto one = [&](auto j_c) __attribute__((always_inline)) {  // (as a function with a result: a break behind each made the compiler spill)
+                    constexpr int J = decltype(j_c)::value;
+                    if (s > o_hi) return false;
+                    iteration(s, J, [&](uint32_t, uint32_t) __attribute__((always_inline)) {
+                        work(s, J & 1 ? sb : sa, J & 1 ? sa : sb, J & 1 ? pa : pb, J & 1 ? pb : pa, (J + 1) % S * F::SLOT, (J + S - 1) % S * F::SLOT, (J + 2) % S * F::SLOT, J * F::SLOT);
+                    });
+                    ++s;
+                    return true;
+                };
+                if (!one(std::integral_constant<int, 0>{})) break;
+                if (!one(std::integral_constant<int, 1>{})) break;
+                if constexpr (S == 4) {
+                    if (!one(std::integral_constant<int, 2>{})) break;
+                    if (!one(std::integral_constant<int, 3>{})) break;
+                }
+            }
         }
-        wait_vm0_and_sync();
+        j = (s - s_lo) % S;
+        idle(s_hi + 1);
+        wait_vm0_and_sync();  // (the requests past the last step write zeros)
     }
-    store_output<D>(p, ot, m2, lsum, 0, head, qrow, hh);
+
+    // ---- the groups add their sums, each for its share of the features
+    float l = xhalf_sum(lsum);
+    float m = m2, w_own = 1.f;
+    if constexpr (KQ == 2) {
+        float* const ex = reinterpret_cast<float*>(smem);                    // [wave][unit of 4 registers][lane][4]
+        float* const xml = reinterpret_cast<float*>(smem + 4 * D * 64);      // [wave][max, l][32 rows]
+        if (hh == 0) {
+            xml[wave * 64 + ql] = m2;
+            xml[wave * 64 + 32 + ql] = l;
+        }
+        // group 0 keeps the first half of the features' blocks of 32, group 1 the second
+#pragma unroll
+        for (int db = 0; db < DB / 2; ++db)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const f32x16& o = kq == 0 ? ot[DB / 2 + db] : ot[db];
+                *reinterpret_cast<f32x4*>(ex + ((wave * (DB / 2 * 4) + db * 4 + q) * 64 + lane) * 4) = f32x4{o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]};
+            }
+        __syncthreads();
+        const int other = wave ^ RW;  // (wave = kq * RW + rw)
+        const float mo = xml[other * 64 + ql], lo = xml[other * 64 + 32 + ql];
+        m = fmaxf(m2, mo);
+        const float msub = finite_max(m);
+        w_own = __builtin_amdgcn_exp2f(m2 - msub);
+        const float w_other = __builtin_amdgcn_exp2f(mo - msub);
+        l = w_own * l + w_other * lo;
+#pragma unroll
+        for (int db = 0; db < DB / 2; ++db)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const f32x4 x = *reinterpret_cast<const f32x4*>(ex + ((other * (DB / 2 * 4) + db * 4 + q) * 64 + lane) * 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float mine = kq == 0 ? ot[db][4 * q + e] : ot[DB / 2 + db][4 * q + e];
+                    ot[db][4 * q + e] = __builtin_fmaf(w_own, mine, w_other * x[e]);
+                }
+            }
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if (qrow < N && p.LSE && kq == 0 && hh == 0) p.LSE[(size_t)head * N + qrow] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    uint16_t* const Og = p.O + ((size_t)head * N + qrow_c) * D + (KQ == 2 ? kq * (D / 2) : 0);
+#pragma unroll
+    for (int db = 0; db < DB / KQ; ++db)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            // the lane pair (l, l ^ 32) trades runs of four features for runs of eight, as in store_output
+            const f32x16& o = ot[db];
+            const int e = 8 * u;
+            const uint32_t a0 = pack_bf16(o[e] * inv, o[e + 1] * inv), a1 = pack_bf16(o[e + 2] * inv, o[e + 3] * inv);
+            const uint32_t b0 = pack_bf16(o[e + 4] * inv, o[e + 5] * inv), b1 = pack_bf16(o[e + 6] * inv, o[e + 7] * inv);
+            const auto r0 = __builtin_amdgcn_permlane32_swap(a0, b0, false, false);
+            const auto r1 = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
+            if (qrow < N) *reinterpret_cast<u32x4*>(Og + 32 * db + 16 * u + 8 * hh) = u32x4{r0[0], r1[0], r0[1], r1[1]};
+        }
 }
 
 }  // namespace

@@ -190,7 +190,10 @@ int vfa_masked_attn_fwd(const void* Q, const void* K, const void* V, void* O, fl
     if (!aligned8(ranges) || !aligned4(slopes) || !aligned4(LSE)) return VFA_ERR_INVALID_ARG;
     if (B == 0 || N == 0) return VFA_OK;
     if (!Q || !K || !V || !O || !aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O)) return VFA_ERR_INVALID_ARG;
-    const long long blocks = ((long long)N + 127) / 128, heads = (long long)B * Hq;
+    const int n_cu = cu_count() > 0 ? cu_count() : 256;
+    const long long heads = (long long)B * Hq;
+    const bool split = heads * (((long long)N + 127) / 128) < 2LL * n_cu;
+    const long long rows = split ? 64 : 128, blocks = ((long long)N + rows - 1) / rows;
     if ((long long)N * 2 * d > 0x7fffffffLL || heads > 0x7fffffffLL / blocks || heads * blocks > kMaxWorkgroups256) return VFA_ERR_UNSUPPORTED;
     MaskedParams P{};
     Params& p = P.a;
@@ -201,16 +204,21 @@ int vfa_masked_attn_fwd(const void* Q, const void* K, const void* V, void* O, fl
     p.c = scale * kLog2e;
     P.s = scores_of(slopes, score_cap, scale);
     P.ranges = reinterpret_cast<const int2*>(ranges);
-    P.unit = 1.f / scale;
     const unsigned grid = (unsigned)(heads * blocks);
     (void)hipGetLastError();
     with_d(d, [&](auto d_c) {
         constexpr int D = decltype(d_c)::value;
         hipStream_t s = (hipStream_t)stream;
-        if (score_cap > 0.f && slopes) attn_masked_kernel<D, true, true><<<grid, 256, 0, s>>>(P);
-        else if (score_cap > 0.f) attn_masked_kernel<D, true, false><<<grid, 256, 0, s>>>(P);
-        else if (slopes) attn_masked_kernel<D, false, true><<<grid, 256, 0, s>>>(P);
-        else attn_masked_kernel<D, false, false><<<grid, 256, 0, s>>>(P);
+        auto launch = [&](auto cap_c, auto bias_c) {
+            constexpr bool CAP = decltype(cap_c)::value, BIAS = decltype(bias_c)::value;
+            if (split) attn_masked_kernel<D, 2, 2, CAP, BIAS><<<grid, 256, 0, s>>>(P);
+            else attn_masked_kernel<D, 4, 1, CAP, BIAS><<<grid, 256, 0, s>>>(P);
+        };
+        using std::false_type, std::true_type;
+        if (score_cap > 0.f && slopes) launch(true_type{}, true_type{});
+        else if (score_cap > 0.f) launch(true_type{}, false_type{});
+        else if (slopes) launch(false_type{}, true_type{});
+        else launch(false_type{}, false_type{});
     });
     return launched();
 }
