@@ -7,7 +7,7 @@ namespace {
 
 // ---------------------------------------------------------------------------------------------
 // Row i sees the keys [lo, hi) of its entry in `ranges` (all without one), and with `causal` none behind itself.  A workgroup has 32 RW rows of a head and
-// goes over the steps of 32 KQ keys from the first key that any of its rows sees to the last; wave (rw, kq) multiplies the 32 keys of group kq with
+// goes over the steps of 32 KQ keys from the last key that any of its rows sees to the first (a bias then leaves the max where the first steps put it); wave (rw, kq) multiplies the 32 keys of group kq with
 // rows 32 rw .. 32 rw + 31, and leaves out the steps at either end that none of its own rows sees.
 //
 // A score's log2 weight is A + F v.  Without a cap v is what the matrix unit gives and F = c; with one v = 1 / (1 + e^(2 s / cap)), F = -2 cap2 and A = cap2 (see
@@ -102,9 +102,10 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
         wg_all_lo = wave_fold(max(r0.x, r1.x), larger);
         wg_all_hi = wave_fold(min(r0.y, r1.y), lesser);
     }
-    const int s_lo = wg_lo < wg_hi ? wg_lo / KT : 0, s_hi = wg_lo < wg_hi ? (wg_hi + KT - 1) / KT : 0;
-    // steps of the wave: [o_lo, o_hi)
-    const int o_lo = any_lo < any_hi ? max((any_lo - 32 * kq - 31 + KT - 1) / KT, s_lo) : s_hi, o_hi = any_hi > 32 * kq ? (any_hi - 32 * kq + KT - 1) / KT : 0;
+    // Blocks of KT keys [b_lo, b_hi): a step each, the last block first.  Steps of the wave: [o_lo, o_hi)
+    const int b_lo = wg_lo < wg_hi ? wg_lo / KT : 0, b_hi = wg_lo < wg_hi ? (wg_hi + KT - 1) / KT : 0, steps = b_hi - b_lo;
+    const int o_lo = any_hi > 32 * kq ? b_hi - (any_hi - 32 * kq + KT - 1) / KT : steps;
+    const int o_hi = any_lo < any_hi ? b_hi - max((any_lo - 32 * kq - 31 + KT - 1) / KT, b_lo) : 0;
 
     // ---- requests: a wave moves LI adjacent pieces (1 KiB of whole rows) of a slot, by buffer loads whose buffer is the head's keys: rows past the end
     // of the sequence are out of its range and LDS gets zeros, as for steps before the first one and past the last
@@ -117,7 +118,7 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
     const uint32_t bytes = (uint32_t)N * T::ROWB;  // (launched for fewer than 2^31)
     const u32x4 rsrcK = tile_buffer((uint64_t)(uintptr_t)(p.K + (size_t)kv * N * D), bytes), rsrcV = tile_buffer((uint64_t)(uintptr_t)(p.V + (size_t)kv * N * D), bytes);
     auto request = [&](const u32x4& rsrc, int s, int slot, bool is_v) __attribute__((always_inline)) {
-        const uint32_t at = s >= s_lo && s < s_hi ? (uint32_t)s * F::SLOT : bytes, to = lds0 + slot * F::SLOT;
+        const uint32_t at = (uint32_t)s < (uint32_t)steps ? (uint32_t)(b_hi - 1 - s) * F::SLOT : bytes, to = lds0 + slot * F::SLOT;
         if constexpr (LI == 4) request4_at(rsrc, at, is_v ? offV : offK[0], is_v ? offV : offK[1], is_v ? offV : offK[2], is_v ? offV : offK[3], to);
         else if constexpr (LI == 2) request2_at(rsrc, at, is_v ? offV : offK[0], is_v ? offV : offK[1], to);
         else request1_at(rsrc, at, is_v ? offV : offK[0], to);
@@ -128,12 +129,12 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
     for (int db = 0; db < DB; ++db) ot[db] = f32x16{0};
     float m2 = -INFINITY, lsum = 0.f;
 
-    if (s_lo < s_hi) {  // (the same in all waves)
-        // slot of step s: (s - s_lo) mod S.  The first iteration takes the last slot of V for that of the step before it: zeros
+    if (steps > 0) {  // (the same in all waves)
+        // slot of step s: s mod S.  The first iteration takes the last slot of V for that of the step before it: zeros
 #pragma unroll
-        for (int e = 0; e < S - 1; ++e) request(rsrcK, s_lo + e, e, false);
+        for (int e = 0; e < S - 1; ++e) request(rsrcK, e, e, false);
 #pragma unroll
-        for (int e = 0; e < S - 3; ++e) request(rsrcV, s_lo + e, S + e, true);
+        for (int e = 0; e < S - 3; ++e) request(rsrcV, e, S + e, true);
 #pragma unroll
         for (int u = 0; u < LI; ++u) *reinterpret_cast<u32x4*>(Vs + (S - 1) * F::SLOT + (wave * LI + u) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
         {
@@ -170,18 +171,19 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
         };
         // (all in steps, worked out once) Sides of a bias: the wave's keys of step s all at or before all of its rows; all at or behind all of them.
         // Steps that all rows of the wave see whole, and all rows of the workgroup
-        const int l_hi = qrow0 >= 32 * kq + 31 ? (qrow0 - 32 * kq - 31) / KT + 1 : 0, r_lo = (max(qrow0 + 31 - 32 * kq, 0) + KT - 1) / KT;
-        const int w_lo = (max(all_lo - 32 * kq, 0) + KT - 1) / KT, w_hi = all_hi >= 32 * kq + 32 ? (all_hi - 32 * kq - 32) / KT + 1 : 0;
-        const int f_lo = (wg_all_lo + KT - 1) / KT, f_hi = wg_all_hi / KT;
-        auto left = [&](int s) { return !BIAS || s < l_hi; };
-        auto right = [&](int s) { return s >= r_lo; };
-        auto whole = [&](int s) { return s >= w_lo && s < w_hi; };
+        const int l_lo = b_hi - (qrow0 >= 32 * kq + 31 ? (qrow0 - 32 * kq - 31) / KT + 1 : 0), r_hi = b_hi - (max(qrow0 + 31 - 32 * kq, 0) + KT - 1) / KT;
+        const int w_lo = b_hi - (all_hi >= 32 * kq + 32 ? (all_hi - 32 * kq - 32) / KT + 1 : 0), w_hi = b_hi - (max(all_lo - 32 * kq, 0) + KT - 1) / KT;
+        const int f_lo = b_hi - wg_all_hi / KT, f_hi = b_hi - (wg_all_lo + KT - 1) / KT;
+        const uint32_t w_many = max(w_hi - w_lo, 0), f_many = max(f_hi - f_lo, 0);
+        auto left = [&](int s) { return !BIAS || s >= l_lo; };
+        auto right = [&](int s) { return s < r_hi; };
+        auto whole = [&](int s) { return (uint32_t)(s - w_lo) < w_many; };
+        auto first_key = [&](int s) { return (b_hi - 1 - s) * KT + 32 * kq; };  // of the wave
 
         // the softmax of a step, in parts: pairs of scores to v (CAP), the max, pairs of v to weights
-        float add, alpha;   // A - the max; what the sums so far are to be multiplied with
-        bool moved;         // (of the wave)
+        float add = -INFINITY;  // A - the max
         auto offset = [&](int s) __attribute__((always_inline)) {  // A
-            const int away = qrow - s * KT - 32 * kq - 4 * hh;
+            const int away = qrow - first_key(s) - 4 * hh;
             const float base = BIAS ? slope2 * (float)(left(s) ? -away : away) : 0.f;
             return CAP ? P.s.cap2 + base : base;
         };
@@ -192,7 +194,9 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
                 if (BIAS) st[e] = __builtin_fmaf(left(s) ? lin : -lin, (float)(8 * (e >> 2) + (e & 3)), st[e]);
             }
         };
-        auto part_m = [&](const f32x16& st, int s) __attribute__((always_inline)) {
+        // Products of po that have been started are in ot, those to come take the changed po: the max may move between any two of them.  It moves by whole
+        // numbers, so that weights in bf16 are rescaled exactly.  (Each row by itself: what the others see changes none of its bits.)
+        auto part_m = [&](const f32x16& st, uint32_t* po, int s) __attribute__((always_inline)) {
             float x = st[0];
 #pragma unroll
             for (int q = 0; q < 7; ++q) x = CAP ? fminf(fminf(x, st[1 + 2 * q]), st[2 + 2 * q]) : fmaxf(fmaxf(x, st[1 + 2 * q]), st[2 + 2 * q]);
@@ -200,13 +204,18 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
             const float a = offset(s), y = __builtin_fmaf(x, fac, a);  // (A differs between the halves)
             const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
             const float top = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
-            const bool up = top > m2;  // (each row by itself: what the others see changes none of its bits)
-            moved = __builtin_amdgcn_ballot_w64(up) != 0;
-            const float m_new = up ? top + kMaskedKeep : m2, msub = finite_max(m_new);
-            alpha = __builtin_amdgcn_exp2f(m2 - msub);
-            lsum *= alpha;
-            m2 = m_new;
-            add = a - msub;
+            if (__builtin_expect(__builtin_amdgcn_ballot_w64(top > m2) != 0, 0)) {
+                const float m_new = top > m2 ? ceilf(top) + kMaskedKeep : m2;
+                const float alpha = ldexpf(1.f, (int)fmaxf(m2 - finite_max(m_new), -1000.f));
+                lsum *= alpha;
+#pragma unroll
+                for (int db = 0; db < DB; ++db) ot[db] *= alpha;
+#pragma unroll
+                for (int q = 0; q < 8; ++q) po[q] = pack_bf16(__uint_as_float(po[q] << 16) * alpha, __uint_as_float(po[q] & 0xffff0000u) * alpha);
+                m2 = m_new;
+                if (!BIAS) add = a - finite_max(m2);
+            }
+            if (BIAS) add = a - finite_max(m2);
         };
         auto part_b = [&](const f32x16& st, uint32_t* pk, int q) __attribute__((always_inline)) {
             const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(st[2 * q], fac, add)), e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(st[2 * q + 1], fac, add));
@@ -215,17 +224,11 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
             pk[q] = pack_bf16(e0, e1);
             asm volatile("" : "+v"(pk[q]), "+v"(lsum));  // (here, between the products: the compiler sank them behind the next branch)
         };
-        auto rescale = [&]() __attribute__((always_inline)) {
-            if (moved) {
-#pragma unroll
-                for (int db = 0; db < DB; ++db) ot[db] *= alpha;
-            }
-        };
         constexpr int R = F::R;
         static_assert(!F::AHEAD || 2 * KK % R == 0, "a step ends where the ring of fragments began");
         bf16x8 fr[R];
         // Iteration s: st, pk of step s; sn of step s + 1, po of step s - 1
-        auto work = [&](int s, f32x16& st, f32x16& sn, uint32_t* pk, const uint32_t* po, uint32_t slot_k, uint32_t slot_v, uint32_t next_k, uint32_t next_v) __attribute__((always_inline)) {
+        auto work = [&](int s, f32x16& st, f32x16& sn, uint32_t* pk, uint32_t* po, uint32_t slot_k, uint32_t slot_v, uint32_t next_k, uint32_t next_v) __attribute__((always_inline)) {
             constexpr bool A = CAP || BIAS;
             constexpr int M = 2 * KK, H = A ? M / 2 : 0;  // products; those in front of the masks
             static_assert(KK == 2 * DB, "as many products on either side");
@@ -252,7 +255,7 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
                 for (int u = 8 * e / H; u < 8 * (e + 1) / H; ++u) part_a(st, s, u);
                 product(e);
             }
-            const int key0 = s * KT + 32 * kq + 4 * hh;
+            const int key0 = first_key(s) + 4 * hh;
             if (BIAS && !left(s) && !right(s)) {  // (part_a counts the distance as if on the right)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) st[r] = __builtin_fmaf(-2.f * lin, fmaxf((float)(qrow - key0 - 8 * (r >> 2) - (r & 3)), 0.f), st[r]);
@@ -267,14 +270,13 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
             for (int e = H; e < M; ++e) {
 #pragma unroll
                 for (int u = 10 * (e - H) / (M - H); u < 10 * (e - H + 1) / (M - H); ++u) {
-                    if (u == 0) part_m(st, s);
+                    if (u == 0) part_m(st, po, s);
                     else if (u >= 2) part_b(st, pk, u - 2);
                 }
                 product(e);
             }
-            rescale();
         };
-        // What surrounds the work of an iteration; j = s - s_lo (mod S)
+        // What surrounds the work of an iteration; j = s mod S
         uint64_t keys = 0;  // of the step whose values are multiplied: those with values that are not finite
         auto iteration = [&](int s, int j, auto f) __attribute__((always_inline)) {
             const uint32_t slot_v = (j + S - 1) % S * F::SLOT;
@@ -282,7 +284,7 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
             // are cleared before the first of them is read
             const int c = F::AHEAD ? s : s - 1;
             uint64_t found = 0;
-            if (c >= s_lo && c < s_hi && !(c >= f_lo && c < f_hi)) {
+            if ((uint32_t)(c - f_lo) >= f_many && (uint32_t)c < (uint32_t)steps) {
                 bad[wave] = clear_not_finite<D, LI>(Vs + (F::AHEAD ? j * F::SLOT : slot_v), wave * LI, lane);
                 __syncthreads();
                 found = bad[0] | bad[1] | bad[2] | bad[3];
@@ -297,7 +299,7 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
                 // (the max may have moved behind the product: what is added is not finite, whatever it is multiplied with)
 #pragma unroll 1
                 for (uint64_t left_over = keys >> (32 * kq) & 0xffffffffull; left_over; left_over &= left_over - 1) {
-                    const int k = (s - 1) * KT + 32 * kq + __builtin_ctzll(left_over);  // (a key of the sequence: behind its end LDS has zeros)
+                    const int k = first_key(s - 1) + __builtin_ctzll(left_over);  // (a key of the sequence: behind its end LDS has zeros)
                     add_not_finite<D>(Vg + (size_t)k * D, k >= own.x && k < own.y, ot, hh);
                 }
             }
@@ -310,15 +312,15 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
         // one before.  What is not the wave's among their steps is masked, so its weights are 0, and the values that they meet are finite: cleared, or,
         // in the first iteration of all, the slot of zeros.
         const bool any = o_lo < o_hi;
-        const int front = any ? s_lo + (o_lo - s_lo) / S * S : s_hi + 2;
-        int s = s_lo - 1, j = S - 1;
+        const int front = any ? o_lo / S * S : steps + 2;
+        int s = -1, j = S - 1;
         auto idle = [&](int end) __attribute__((always_inline)) {
             for (; s < end; ++s) {
                 iteration(s, j, [](uint32_t, uint32_t) {});
                 j = j + 1 == S ? 0 : j + 1;
             }
         };
-        idle(min(front - 1, s_hi + 1));
+        idle(min(front - 1, steps + 1));
         if (any) {
             f32x16 sa, sb;
             uint32_t pa[8], pb[8];
@@ -353,8 +355,8 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
                 }
             }
         }
-        j = (s - s_lo) % S;
-        idle(s_hi + 1);
+        j = s % S;
+        idle(steps + 1);
         wait_vm0_and_sync();  // (the requests past the last step write zeros)
     }
 
