@@ -117,8 +117,8 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(smem) + wave * LI * 1024);
     const uint32_t bytes = (uint32_t)N * T::ROWB;  // (launched for fewer than 2^31)
     const u32x4 rsrcK = tile_buffer((uint64_t)(uintptr_t)(p.K + (size_t)kv * N * D), bytes), rsrcV = tile_buffer((uint64_t)(uintptr_t)(p.V + (size_t)kv * N * D), bytes);
-    auto request = [&](const u32x4& rsrc, int s, int slot, bool is_v) __attribute__((always_inline)) {
-        const uint32_t at = (uint32_t)s < (uint32_t)steps ? (uint32_t)(b_hi - 1 - s) * F::SLOT : bytes, to = lds0 + slot * F::SLOT;
+    auto request = [&](const u32x4& rsrc, int s, int slot, bool is_v, bool there) __attribute__((always_inline)) {
+        const uint32_t at = there || (uint32_t)s < (uint32_t)steps ? (uint32_t)(b_hi - 1 - s) * F::SLOT : bytes, to = lds0 + slot * F::SLOT;
         if constexpr (LI == 4) request4_at(rsrc, at, is_v ? offV : offK[0], is_v ? offV : offK[1], is_v ? offV : offK[2], is_v ? offV : offK[3], to);
         else if constexpr (LI == 2) request2_at(rsrc, at, is_v ? offV : offK[0], is_v ? offV : offK[1], to);
         else request1_at(rsrc, at, is_v ? offV : offK[0], to);
@@ -132,9 +132,9 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
     if (steps > 0) {  // (the same in all waves)
         // slot of step s: s mod S.  The first iteration takes the last slot of V for that of the step before it: zeros
 #pragma unroll
-        for (int e = 0; e < S - 1; ++e) request(rsrcK, e, e, false);
+        for (int e = 0; e < S - 1; ++e) request(rsrcK, e, e, false, false);
 #pragma unroll
-        for (int e = 0; e < S - 3; ++e) request(rsrcV, e, S + e, true);
+        for (int e = 0; e < S - 3; ++e) request(rsrcV, e, S + e, true, false);
 #pragma unroll
         for (int u = 0; u < LI; ++u) *reinterpret_cast<u32x4*>(Vs + (S - 1) * F::SLOT + (wave * LI + u) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
         {
@@ -182,26 +182,26 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
 
         // the softmax of a step, in parts: pairs of scores to v (CAP), the max, pairs of v to weights
         float add = -INFINITY;  // A - the max
-        auto offset = [&](int s) __attribute__((always_inline)) {  // A
+        auto offset = [&](int s, bool on_left) __attribute__((always_inline)) {  // A
             const int away = qrow - first_key(s) - 4 * hh;
-            const float base = BIAS ? slope2 * (float)(left(s) ? -away : away) : 0.f;
+            const float base = BIAS ? slope2 * (float)(on_left ? -away : away) : 0.f;
             return CAP ? P.s.cap2 + base : base;
         };
-        auto part_a = [&](f32x16& st, int s, int q) __attribute__((always_inline)) {
+        auto part_a = [&](f32x16& st, bool on_left, int q) __attribute__((always_inline)) {
 #pragma unroll
             for (int e = 2 * q; e < 2 * q + 2; ++e) {
                 if (CAP) st[e] = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(st[e] * P.s.capk));
-                if (BIAS) st[e] = __builtin_fmaf(left(s) ? lin : -lin, (float)(8 * (e >> 2) + (e & 3)), st[e]);
+                if (BIAS) st[e] = __builtin_fmaf(on_left ? lin : -lin, (float)(8 * (e >> 2) + (e & 3)), st[e]);
             }
         };
         // Products of po that have been started are in ot, those to come take the changed po: the max may move between any two of them.  It moves by whole
         // numbers, so that weights in bf16 are rescaled exactly.  (Each row by itself: what the others see changes none of its bits.)
-        auto part_m = [&](const f32x16& st, uint32_t* po, int s) __attribute__((always_inline)) {
+        auto part_m = [&](const f32x16& st, uint32_t* po, int s, bool on_left) __attribute__((always_inline)) {
             float x = st[0];
 #pragma unroll
             for (int q = 0; q < 7; ++q) x = CAP ? fminf(fminf(x, st[1 + 2 * q]), st[2 + 2 * q]) : fmaxf(fmaxf(x, st[1 + 2 * q]), st[2 + 2 * q]);
             x = CAP ? fminf(x, st[15]) : fmaxf(x, st[15]);
-            const float a = offset(s), y = __builtin_fmaf(x, fac, a);  // (A differs between the halves)
+            const float a = offset(s, on_left), y = __builtin_fmaf(x, fac, a);  // (A differs between the halves)
             const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
             const float top = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
             if (__builtin_expect(__builtin_amdgcn_ballot_w64(top > m2) != 0, 0)) {
@@ -228,8 +228,9 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
         static_assert(!F::AHEAD || 2 * KK % R == 0, "a step ends where the ring of fragments began");
         bf16x8 fr[R];
         // Iteration s: st, pk of step s; sn of step s + 1, po of step s - 1
-        auto work = [&](int s, f32x16& st, f32x16& sn, uint32_t* pk, uint32_t* po, uint32_t slot_k, uint32_t slot_v, uint32_t next_k, uint32_t next_v) __attribute__((always_inline)) {
-            constexpr bool A = CAP || BIAS;
+        auto work = [&](int s, f32x16& st, f32x16& sn, uint32_t* pk, uint32_t* po, uint32_t slot_k, uint32_t slot_v, uint32_t next_k, uint32_t next_v, auto plain_c)
+                        __attribute__((always_inline)) {
+            constexpr bool A = CAP || BIAS, PLAIN = decltype(plain_c)::value;
             constexpr int M = 2 * KK, H = A ? M / 2 : 0;  // products; those in front of the masks
             static_assert(KK == 2 * DB, "as many products on either side");
             auto frag = [&](int e, uint32_t sk, uint32_t sv) __attribute__((always_inline)) { return e & 1 ? ld_v(sv, e >> 1) : ld_k(sk, e >> 1); };
@@ -252,15 +253,15 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
 #pragma unroll
             for (int e = 0; e < H; ++e) {
 #pragma unroll
-                for (int u = 8 * e / H; u < 8 * (e + 1) / H; ++u) part_a(st, s, u);
+                for (int u = 8 * e / H; u < 8 * (e + 1) / H; ++u) part_a(st, PLAIN || left(s), u);
                 product(e);
             }
             const int key0 = first_key(s) + 4 * hh;
-            if (BIAS && !left(s) && !right(s)) {  // (part_a counts the distance as if on the right)
+            if (BIAS && !PLAIN && !left(s) && !right(s)) {  // (part_a counts the distance as if on the right)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) st[r] = __builtin_fmaf(-2.f * lin, fmaxf((float)(qrow - key0 - 8 * (r >> 2) - (r & 3)), 0.f), st[r]);
             }
-            if (!whole(s)) {
+            if (!PLAIN && !whole(s)) {
                 const uint32_t first = own.x - key0, many = own.y - own.x;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) st[r] = (uint32_t)(8 * (r >> 2) + (r & 3)) - first < many ? st[r] : CAP ? INFINITY : -INFINITY;
@@ -270,7 +271,7 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
             for (int e = H; e < M; ++e) {
 #pragma unroll
                 for (int u = 10 * (e - H) / (M - H); u < 10 * (e - H + 1) / (M - H); ++u) {
-                    if (u == 0) part_m(st, po, s);
+                    if (u == 0) part_m(st, po, s, PLAIN || left(s));
                     else if (u >= 2) part_b(st, pk, u - 2);
                 }
                 product(e);
@@ -278,23 +279,24 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
         };
         // What surrounds the work of an iteration; j = s mod S
         uint64_t keys = 0;  // of the step whose values are multiplied: those with values that are not finite
-        auto iteration = [&](int s, int j, auto f) __attribute__((always_inline)) {
+        auto iteration = [&](int s, int j, auto plain_c, auto f) __attribute__((always_inline)) {
+            constexpr bool PLAIN = decltype(plain_c)::value;
             const uint32_t slot_v = (j + S - 1) % S * F::SLOT;
             // No row of the workgroup may get what is not finite among the values of a key that it does not see: those of a step that not all rows see whole
             // are cleared before the first of them is read
             const int c = F::AHEAD ? s : s - 1;
             uint64_t found = 0;
-            if ((uint32_t)(c - f_lo) >= f_many && (uint32_t)c < (uint32_t)steps) {
+            if (!PLAIN && (uint32_t)(c - f_lo) >= f_many && (uint32_t)c < (uint32_t)steps) {
                 bad[wave] = clear_not_finite<D, LI>(Vs + (F::AHEAD ? j * F::SLOT : slot_v), wave * LI, lane);
                 __syncthreads();
                 found = bad[0] | bad[1] | bad[2] | bad[3];
                 found = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(found >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)found);
             }
             if (!F::AHEAD) keys = found;
-            request(rsrcK, s + S, j % S, false);
-            request(rsrcV, s - 2 + S, S + (j + S - 2) % S, true);
+            request(rsrcK, s + S, j % S, false, PLAIN);
+            request(rsrcV, s - 2 + S, S + (j + S - 2) % S, true, PLAIN);
             f((j + 1) % S * F::SLOT, slot_v);
-            if (__builtin_expect(keys != 0, 0)) {
+            if (!PLAIN && __builtin_expect(keys != 0, 0)) {
                 const uint16_t* const Vg = p.V + (size_t)kv * N * D;
                 // (the max may have moved behind the product: what is added is not finite, whatever it is multiplied with)
 #pragma unroll 1
@@ -303,7 +305,7 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
                     add_not_finite<D>(Vg + (size_t)k * D, k >= own.x && k < own.y, ot, hh);
                 }
             }
-            keys = found;
+            if (!PLAIN) keys = found;
             // K of step s + 2 and V of step s are there, AHEAD those of the steps behind them; reads of slots that are written next are through with their products
             __builtin_amdgcn_s_waitcnt(F::AHEAD ? 0x0F70 | 2 * LI : 0x0070);
             __builtin_amdgcn_s_barrier();
@@ -316,7 +318,7 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
         int s = -1, j = S - 1;
         auto idle = [&](int end) __attribute__((always_inline)) {
             for (; s < end; ++s) {
-                iteration(s, j, [](uint32_t, uint32_t) {});
+                iteration(s, j, std::false_type{}, [](uint32_t, uint32_t) {});
                 j = j + 1 == S ? 0 : j + 1;
             }
         };
@@ -326,7 +328,7 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
             uint32_t pa[8], pb[8];
 #pragma unroll
             for (int q = 0; q < 8; ++q) pa[q] = 0;
-            iteration(s, S - 1, [&](uint32_t, uint32_t) __attribute__((always_inline)) {
+            iteration(s, S - 1, std::false_type{}, [&](uint32_t, uint32_t) __attribute__((always_inline)) {
                 sa = f32x16{0};
 #pragma unroll
                 for (int kk = 0; kk < KK; ++kk) sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_k(0, kk), qf[kk], sa, 0, 0, 0);
@@ -337,14 +339,34 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
                 }
             });
             ++s;
+            auto step = [&](auto j_c, auto plain_c) __attribute__((always_inline)) {
+                constexpr int J = decltype(j_c)::value;
+                iteration(s, J, plain_c, [&](uint32_t, uint32_t) __attribute__((always_inline)) {
+                    work(s, J & 1 ? sb : sa, J & 1 ? sa : sb, J & 1 ? pa : pb, J & 1 ? pb : pa, (J + 1) % S * F::SLOT, (J + S - 1) % S * F::SLOT, (J + 2) % S * F::SLOT, J * F::SLOT, plain_c);
+                });
+                ++s;
+            };
+            auto round = [&](auto plain_c) __attribute__((always_inline)) {
+                step(std::integral_constant<int, 0>{}, plain_c);
+                step(std::integral_constant<int, 1>{}, plain_c);
+                if constexpr (S == 4) {
+                    step(std::integral_constant<int, 2>{}, plain_c);
+                    step(std::integral_constant<int, 3>{}, plain_c);
+                }
+            };
+            // Whole rounds of steps with nothing special, [plain_lo, plain_hi), have a loop without a condition: all rows of the wave see them whole, on the left,
+            // those of the workgroup the step whose values are read first (and the one before), and there is a step to request
+            int plain_lo = max(max(w_lo, f_lo + 1), front), plain_hi = min(min(w_hi, f_hi), min(steps - S, o_hi));
+            if (BIAS) plain_lo = max(plain_lo, l_lo);
+            plain_lo = (plain_lo + S - 1) / S * S;
+            if (plain_hi - plain_lo >= S) {
+                while (s < plain_lo) round(std::false_type{});
+                while (s + S <= plain_hi) round(std::true_type{});
+            }
             for (;;) {
                 auto one = [&](auto j_c) __attribute__((always_inline)) {  // (as a function with a result: a break behind each made the compiler spill)
-                    constexpr int J = decltype(j_c)::value;
                     if (s > o_hi) return false;
-                    iteration(s, J, [&](uint32_t, uint32_t) __attribute__((always_inline)) {
-                        work(s, J & 1 ? sb : sa, J & 1 ? sa : sb, J & 1 ? pa : pb, J & 1 ? pb : pa, (J + 1) % S * F::SLOT, (J + S - 1) % S * F::SLOT, (J + 2) % S * F::SLOT, J * F::SLOT);
-                    });
-                    ++s;
+                    step(j_c, std::false_type{});
                     return true;
                 };
                 if (!one(std::integral_constant<int, 0>{})) break;
