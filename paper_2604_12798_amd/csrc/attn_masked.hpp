@@ -52,7 +52,7 @@ struct Masked {
     static constexpr int S = KQ == 1 ? 4 : 2;          // slots of each
     static constexpr int LI = SLOT / 4096;             // load instructions of a wave and slot
     static constexpr bool AHEAD = S == 4;              // slots are there a step early, and a step's first fragments are read in the one before
-    static constexpr int R = !AHEAD ? 3 : D == 128 ? 8 : 4;  // fragments under way
+    static constexpr int R = D == 128 ? 8 : 4;  // fragments under way
     static constexpr int LDS_BYTES = 2 * S * SLOT;
     static_assert(RW * KQ == 4, "four waves");
     static_assert(KQ == 1 || 4 * (D * 64 + 256) <= LDS_BYTES, "the partial sums have to fit the slots' memory");

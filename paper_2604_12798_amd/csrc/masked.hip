@@ -87,15 +87,22 @@ int vfa_kvp_append(const void* K, const void* V, void* KP, void* VP, const int* 
     return launched();
 }
 
+// Two tiles a range at least (8 heads of 2048 keys, d = 128: 8 ranges 10.3 us, 16 9.4; of 600 1 12.1, 3 9.9, 4 9.8), one range where there are few.  Equal lengths:
+// as many ranges as compute units, whose workgroups of four waves have a unit each at d = 128 and half of one at d = 64 (32 heads of 32768 keys 4 ranges 96, 6 83, 8
+// 85, 16 87, 32 92; 128 of 4096: 1 55, 2 46, 4 50; 256 of 1000: 1 25.8, 2 30.6; 8 of 8000: 16 14.1, 32 11.8, 48 17.1; d = 64: 16 of 2048 8 8.7, 16 8.1).
+// Lengths of their own, dealt out to workgroups of one wave: as many as the units hold (128 heads of 200 to 8192 keys, d = 128: 4 ranges 55, 6 51, 8 49.5, 12 55, 16 56; with
+// four waves each 2 55, 4 54.6, 8 64.5; 64 of 500 to 16384: 8 49.9, 16 48.4, 24 55.8; d = 64, 128 of 300 to 8192: 8 28, 16 26.9, 24 29.6).
 int vfa_kvp_decode_splits(int B, int Hq, int Hkv, int n_q, int d, int n_keys, int varlen) {
     if (B <= 0 || Hq <= 0 || Hkv <= 0 || n_q <= 0 || n_keys <= 0 || (long long)B * Hkv > 65535) return 1;
     const int n_cu = cu_count() > 0 ? cu_count() : 256, all = n_keys / BN + (n_keys % BN != 0);  // (n_keys + 63 may not fit)
     const long long rows = (long long)(Hq / Hkv) * n_q;
     const int g = Hq / Hkv, tokens = rows <= 32 ? n_q : g < 32 ? 32 / g : 1;
     const long long heads = (long long)B * Hkv * (((long long)n_q + tokens - 1) / tokens);  // (with more than 32 rows, groups of them)
-    if (all <= 8) return 1;
-    const long long n = varlen && B > 1 ? (2LL * n_cu + heads - 1) / heads : n_cu / heads;
-    return (int)max(1LL, min(n, (all + 3) / 4LL));
+    if (all <= (d == 64 ? 8 : 5)) return 1;
+    const bool dealt = varlen && B > 1 && rows <= 32;
+    const long long slots = (long long)n_cu * (d == 64 ? 2 : 1) * (dealt ? 4 : 1);
+    if (dealt && 2 * heads > 3LL * n_cu) return 1;  // (512 heads of 200 to 2048 keys: 1 range of four waves 53.1, 2 of one 55.8)
+    return (int)max(1LL, min(slots / heads, min((all + 1LL) / 2, 4096LL)));
 }
 
 size_t vfa_kvp_decode_workspace_bytes(int B, int Hq, int n_q, int d, int n_splits) {
@@ -144,11 +151,12 @@ int vfa_kvp_decode_fwd(const void* Q, const void* KP, const void* VP, const int*
     const bool dealt = seq_lens && n_splits > 1 && B > 1 && (B <= 64 || (B <= DEAL_MAX_B && (long long)B * Hkv * n_splits <= 8LL * n_cu && ceil_div(n_cap, BN) > 2 * n_splits));
     with_d(d, [&](auto d_c) {
         constexpr int D = decltype(d_c)::value;
+        // (dealt out, there are enough ranges for one wave each)
         auto launch = [&](auto halves_c) {
             constexpr bool HALVES = decltype(halves_c)::value;
             const dim3 grid((unsigned)n_splits, (unsigned)B, (unsigned)Hkv);
             if (!seq_lens) kvp_decode_kernel<D, 4, LENS_ONE, false, HALVES><<<grid, 256, 0, s>>>(P);
-            else if (dealt) kvp_decode_kernel<D, 4, LENS_DEALT, false, HALVES><<<grid, 256, 0, s>>>(P);
+            else if (dealt) kvp_decode_kernel<D, 1, LENS_DEALT, false, HALVES><<<grid, 64, 0, s>>>(P);
             else kvp_decode_kernel<D, 4, LENS_FIXED, false, HALVES><<<dim3((unsigned)n_splits, (unsigned)Hkv, (unsigned)B), 256, 0, s>>>(P);
         };
         if (grouped) {
