@@ -11,8 +11,8 @@ namespace {
 // rows 32 rw .. 32 rw + 31, and leaves out the steps at either end that none of its own rows sees.
 //
 // A score's log2 weight is A + F v.  Without a cap v is what the matrix unit gives and F = c; with one v = 1 / (1 + e^(2 s / cap)), F = -2 cap2 and A = cap2 (see
-// Scores).  A bias -slope |i - j| is linear in the key's place in the step on either side of the row: that part goes into v, one multiply-add with a
-// constant, and the rest is the step's A.
+// Scores).  A bias -slope |i - j| is linear in the key's place in the step on either side of the row: that part goes into v, and the rest is the
+// step's A.
 //
 // Iteration s of a wave: Q.K^T of its step s + 1 and P.V of its step s - 1, a product of each in turn, with the softmax of step s dealt out between them.  (The two
 // waves of a SIMD do not fill each other's gaps: one after the other a tile's products and its vector work took their sum.)  Its max is a reference,
@@ -24,7 +24,22 @@ struct MaskedParams {
     Params a;          // Q, K, V, O, LSE, sizes, items, c
     Scores s;
     const int2* ranges;
+    int together, heads8;  // KV heads of an XCD whose blocks are taken together; KV heads of an XCD, or 0
 };
+
+// The order of the items.  Eights of KV heads have an XCD each, whose L2 then holds their keys, and a list: `together` of its KV heads at a time, late (long) blocks of
+// all of them first, so that no long item starts when the others have ended, but no more heads than fill the XCD twice.  (One head after the other, 4 x 16 heads of 4096, d = 64:
+// the eight heads of an XCD are 256 items in 96 places; the last head's longest starts in the last third and ends 1.35 times the mean, all together 1.1.)
+// Other numbers of KV heads: late blocks of all heads first.
+__device__ __forceinline__ Item masked_item(const MaskedParams& P, int id) {
+    const Params& p = P.a;
+    if (!P.heads8) return item_of(p, id);
+    const int y = id >> 3, per = P.together * p.g * p.Tr, part = y / per;
+    const int k = min(P.together, P.heads8 - part * P.together);  // KV heads of this part of the list
+    const int rem = y - part * per, t = rem / (k * p.g), r = rem - t * k * p.g, j = r / p.g;
+    const int kv = (part * P.together + j) * 8 + (id & 7);
+    return {kv * p.g + r - j * p.g, kv, p.Tr - 1 - t};
+}
 
 template <typename F>
 __device__ __forceinline__ int wave_fold(int x, F f) {
@@ -59,7 +74,7 @@ struct Masked {
 };
 
 template <int D, int RW, int KQ, bool CAP, bool BIAS>
-__global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams P) {
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_masked_kernel(const MaskedParams P) {
     const Params& p = P.a;
     using T = Tile<D>;
     using F = Masked<D, RW, KQ>;
@@ -70,7 +85,7 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
     const int tid = threadIdx.x, lane = tid & 63, ql = lane & 31, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int rw = wave % RW, kq = wave / RW;
-    const auto [head, kv, i] = item_of(p, blockIdx.x);
+    const auto [head, kv, i] = masked_item(P, blockIdx.x);
     const int N = p.N, row0 = i * BM, b = kv / p.Hkv;
     const int qrow0 = row0 + 32 * rw, qrow = qrow0 + ql, qrow_c = min(qrow, N - 1);
     // the keys [x, y) that a row sees; one that sees none has [0, 0)
@@ -180,17 +195,38 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
         auto whole = [&](int s) { return (uint32_t)(s - w_lo) < w_many; };
         auto first_key = [&](int s) { return (b_hi - 1 - s) * KT + 32 * kq; };  // of the wave
 
+        // What a step's scores start from: a bias's part that is linear in the key's place, as one more product, of the places 0 .. 31 (exact in bf16) with the
+        // slope in three pieces of bf16.  (A multiply-add for each score instead: 4 x 16 heads of 4096, d = 64, 201 us, 1xx)
+        bf16x8 places, pieces;
+        if (BIAS && !CAP) {
+            float rest = lin;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                places[e] = (__bf16)(hh == 0 && e < 3 ? (float)ql : 0.f);
+                pieces[e] = (__bf16)(hh == 0 && e < 3 ? rest : 0.f);
+                rest -= (float)pieces[e];
+            }
+        }
+        auto before = [&](bool on_left) __attribute__((always_inline)) -> f32x16 {
+            if (!BIAS || CAP) return f32x16{0};
+            u32x4 b = __builtin_bit_cast(u32x4, pieces);
+            if (!on_left) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) b[e] ^= 0x80008000u;
+            }
+            return __builtin_amdgcn_mfma_f32_32x32x16_bf16(places, __builtin_bit_cast(bf16x8, b), f32x16{0}, 0, 0, 0);
+        };
         // the softmax of a step, in parts: pairs of scores to v (CAP), the max, pairs of v to weights
         float add = -INFINITY;  // A - the max
         auto offset = [&](int s, bool on_left) __attribute__((always_inline)) {  // A
-            const int away = qrow - first_key(s) - 4 * hh;
+            const int away = qrow - first_key(s) - (CAP ? 4 * hh : 0);
             const float base = BIAS ? slope2 * (float)(on_left ? -away : away) : 0.f;
             return CAP ? P.s.cap2 + base : base;
         };
         auto part_a = [&](f32x16& st, bool on_left, int q) __attribute__((always_inline)) {
 #pragma unroll
             for (int e = 2 * q; e < 2 * q + 2; ++e) {
-                if (CAP) st[e] = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(st[e] * P.s.capk));
+                st[e] = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(st[e] * P.s.capk));
                 if (BIAS) st[e] = __builtin_fmaf(on_left ? lin : -lin, (float)(8 * (e >> 2) + (e & 3)), st[e]);
             }
         };
@@ -201,7 +237,7 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
 #pragma unroll
             for (int q = 0; q < 7; ++q) x = CAP ? fminf(fminf(x, st[1 + 2 * q]), st[2 + 2 * q]) : fmaxf(fmaxf(x, st[1 + 2 * q]), st[2 + 2 * q]);
             x = CAP ? fminf(x, st[15]) : fmaxf(x, st[15]);
-            const float a = offset(s, on_left), y = __builtin_fmaf(x, fac, a);  // (A differs between the halves)
+            const float a = offset(s, on_left), y = __builtin_fmaf(x, fac, a);  // (with a cap and a bias A differs between the halves)
             const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
             const float top = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
             if (__builtin_expect(__builtin_amdgcn_ballot_w64(top > m2) != 0, 0)) {
@@ -230,7 +266,7 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
         // Iteration s: st, pk of step s; sn of step s + 1, po of step s - 1
         auto work = [&](int s, f32x16& st, f32x16& sn, uint32_t* pk, uint32_t* po, uint32_t slot_k, uint32_t slot_v, uint32_t next_k, uint32_t next_v, auto plain_c)
                         __attribute__((always_inline)) {
-            constexpr bool A = CAP || BIAS, PLAIN = decltype(plain_c)::value;
+            constexpr bool A = CAP, PLAIN = decltype(plain_c)::value;
             constexpr int M = 2 * KK, H = A ? M / 2 : 0;  // products; those in front of the masks
             static_assert(KK == 2 * DB, "as many products on either side");
             auto frag = [&](int e, uint32_t sk, uint32_t sv) __attribute__((always_inline)) { return e & 1 ? ld_v(sv, e >> 1) : ld_k(sk, e >> 1); };
@@ -239,7 +275,7 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
                     const int f = e >> 1;
                     ot[f % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[e % R], pf(po, f / DB), ot[f % DB], 0, 0, 0);
                 } else {
-                    sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[e % R], qf[e >> 1], e == 0 ? f32x16{0} : sn, 0, 0, 0);
+                    sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[e % R], qf[e >> 1], e == 0 ? before(PLAIN || left(s + 1)) : sn, 0, 0, 0);
                 }
                 if (e + R < M) fr[e % R] = frag(e + R, slot_k, slot_v);
                 else if (F::AHEAD) fr[e % R] = frag(e + R - M, next_k, next_v);
@@ -329,7 +365,7 @@ __global__ __launch_bounds__(256, 2) void attn_masked_kernel(const MaskedParams 
 #pragma unroll
             for (int q = 0; q < 8; ++q) pa[q] = 0;
             iteration(s, S - 1, std::false_type{}, [&](uint32_t, uint32_t) __attribute__((always_inline)) {
-                sa = f32x16{0};
+                sa = before(left(front));
 #pragma unroll
                 for (int kk = 0; kk < KK; ++kk) sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_k(0, kk), qf[kk], sa, 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);

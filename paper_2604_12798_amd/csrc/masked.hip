@@ -200,7 +200,8 @@ int vfa_masked_attn_fwd(const void* Q, const void* K, const void* V, void* O, fl
     if (!Q || !K || !V || !O || !aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O)) return VFA_ERR_INVALID_ARG;
     const int n_cu = cu_count() > 0 ? cu_count() : 256;
     const long long heads = (long long)B * Hq;
-    const bool split = heads * (((long long)N + 127) / 128) < 2LL * n_cu;
+    const int places = (d == 64 ? 3 : 2) * n_cu;  // workgroups that the units hold
+    const bool split = heads * (((long long)N + 127) / 128) < places;
     const long long rows = split ? 64 : 128, blocks = ((long long)N + rows - 1) / rows;
     if ((long long)N * 2 * d > 0x7fffffffLL || heads > 0x7fffffffLL / blocks || heads * blocks > kMaxWorkgroups256) return VFA_ERR_UNSUPPORTED;
     MaskedParams P{};
@@ -212,6 +213,11 @@ int vfa_masked_attn_fwd(const void* Q, const void* K, const void* V, void* O, fl
     p.c = scale * kLog2e;
     P.s = scores_of(slopes, score_cap, scale);
     P.ranges = reinterpret_cast<const int2*>(ranges);
+    if ((B * Hkv) % 8 == 0) {
+        P.heads8 = B * Hkv / 8;
+        const int parts = (int)max(1LL, heads * blocks / (2 * places));
+        P.together = ceil_div(P.heads8, parts);
+    }
     const unsigned grid = (unsigned)(heads * blocks);
     (void)hipGetLastError();
     with_d(d, [&](auto d_c) {
