@@ -104,10 +104,13 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_masked_kernel(const
     const int far = 0x7fffffff;
     // of the wave: the first and the last key that any row sees, and what all rows see; of the workgroup
     int2 own;
+    bf16x8 qf[KK];
     int any_lo, any_hi, all_lo, all_hi, wg_lo, wg_hi, wg_all_lo, wg_all_hi;
     {
         own = range_of(qrow_c);
         const int2 r0 = range_of(min(row0 + lane, N - 1)), r1 = BM == 128 ? range_of(min(row0 + 64 + lane, N - 1)) : r0;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(p.Q + ((size_t)head * N + qrow_c) * D + 16 * kk + 8 * hh);
         any_lo = wave_fold(own.x < own.y ? own.x : far, lesser);
         any_hi = wave_fold(own.y, larger);
         all_lo = wave_fold(own.x, larger);
@@ -138,7 +141,6 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_masked_kernel(const
         else if constexpr (LI == 2) request2_at(rsrc, at, is_v ? offV : offK[0], is_v ? offV : offK[1], to);
         else request1_at(rsrc, at, is_v ? offV : offK[0], to);
     };
-    bf16x8 qf[KK];
     f32x16 ot[DB];
 #pragma unroll
     for (int db = 0; db < DB; ++db) ot[db] = f32x16{0};
@@ -152,11 +154,6 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_masked_kernel(const
         for (int e = 0; e < S - 3; ++e) request(rsrcV, e, S + e, true, false);
 #pragma unroll
         for (int u = 0; u < LI; ++u) *reinterpret_cast<u32x4*>(Vs + (S - 1) * F::SLOT + (wave * LI + u) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
-        {
-            const uint16_t* const Qg = p.Q + ((size_t)head * N + qrow_c) * D;
-#pragma unroll
-            for (int kk = 0; kk < KK; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(Qg + 16 * kk + 8 * hh);
-        }
         const float slope2 = BIAS ? P.s.slopes[head % p.Hq] * kLog2e : 0.f;
         const float fac = CAP ? -2.f * P.s.cap2 : p.c;
         const float lin = BIAS ? slope2 / fac : 0.f;  // the bias of a key's distance, in units of v
@@ -197,11 +194,11 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_masked_kernel(const
 
         // What a step's scores start from: a bias's part that is linear in the key's place, as one more product, of the places 0 .. 31 (exact in bf16) with the
         // slope in three pieces of bf16.  (A multiply-add for each score instead: 4 x 16 heads of 4096, d = 64, 201 us, 1xx)
-        bf16x8 places, pieces;
+        bf16x4 places, pieces;
         if (BIAS && !CAP) {
             float rest = lin;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int e = 0; e < 4; ++e) {
                 places[e] = (__bf16)(hh == 0 && e < 3 ? (float)ql : 0.f);
                 pieces[e] = (__bf16)(hh == 0 && e < 3 ? rest : 0.f);
                 rest -= (float)pieces[e];
@@ -209,12 +206,12 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_masked_kernel(const
         }
         auto before = [&](bool on_left) __attribute__((always_inline)) -> f32x16 {
             if (!BIAS || CAP) return f32x16{0};
-            u32x4 b = __builtin_bit_cast(u32x4, pieces);
+            u32x2 b = __builtin_bit_cast(u32x2, pieces);
             if (!on_left) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) b[e] ^= 0x80008000u;
+                b[0] ^= 0x80008000u;
+                b[1] ^= 0x80008000u;
             }
-            return __builtin_amdgcn_mfma_f32_32x32x16_bf16(places, __builtin_bit_cast(bf16x8, b), f32x16{0}, 0, 0, 0);
+            return __builtin_amdgcn_mfma_f32_32x32x8bf16_1k(__builtin_bit_cast(s16x4, places), __builtin_bit_cast(s16x4, b), f32x16{0}, 0, 0, 0);
         };
         // the softmax of a step, in parts: pairs of scores to v (CAP), the max, pairs of v to weights
         float add = -INFINITY;  // A - the max
@@ -391,11 +388,11 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_masked_kernel(const
                 }
             };
             // Whole rounds of steps with nothing special, [plain_lo, plain_hi), have a loop without a condition: all rows of the wave see them whole, on the left,
-            // those of the workgroup the step whose values are read first (and the one before), and there is a step to request
+            // those of the workgroup the step whose values are read first (and the one before), and there is a step to request.  (Few rows gain nothing from it.)
             int plain_lo = max(max(w_lo, f_lo + 1), front), plain_hi = min(min(w_hi, f_hi), min(steps - S, o_hi));
             if (BIAS) plain_lo = max(plain_lo, l_lo);
             plain_lo = (plain_lo + S - 1) / S * S;
-            if (plain_hi - plain_lo >= S) {
+            if (KQ == 1 && plain_hi - plain_lo >= S) {
                 while (s < plain_lo) round(std::false_type{});
                 while (s + S <= plain_hi) round(std::true_type{});
             }
