@@ -7,17 +7,28 @@ namespace {
 
 // ---------------------------------------------------------------------------------------------
 // Row i sees the keys [lo, hi) of its entry in `ranges` (all without one), and with `causal` none behind itself.  A workgroup has 32 RW rows of a head and
-// goes over the steps of 32 KQ keys from the last key that any of its rows sees to the first (a bias then leaves the max where the first steps put it); wave (rw, kq) multiplies the 32 keys of group kq with
-// rows 32 rw .. 32 rw + 31, and leaves out the steps at either end that none of its own rows sees.
+// goes over the steps of 32 KQ keys from the last key that any of its rows sees to the first (the keys next to a row come first, so that a bias leaves the max where
+// they put it: from the first to the last the max moved in nearly every step, 4 x 16 heads of 4096, d = 64, 293 us, 221 the other way).  Wave (rw, kq) multiplies the
+// 32 keys of group kq with rows 32 rw .. 32 rw + 31, and leaves out the steps at either end that none of its own rows sees.
 //
 // A score's log2 weight is A + F v.  Without a cap v is what the matrix unit gives and F = c; with one v = 1 / (1 + e^(2 s / cap)), F = -2 cap2 and A = cap2 (see
 // Scores).  A bias -slope |i - j| is linear in the key's place in the step on either side of the row: that part goes into v, and the rest is the
 // step's A.
 //
-// Iteration s of a wave: Q.K^T of its step s + 1 and P.V of its step s - 1, a product of each in turn, with the softmax of step s dealt out between them.  (The two
-// waves of a SIMD do not fill each other's gaps: one after the other a tile's products and its vector work took their sum.)  Its max is a reference,
-// the row's max plus kMaskedKeep when it last moved, which moves only when a score passes it.
-// Steps that a wave sees in part, the first and last ones, take the same three parts one after the other.
+// Iteration s of a wave: Q.K^T of its step s + 1 and P.V of its step s - 1, a product of each in turn, with the softmax of step s dealt out between them, and the
+// fragments of the products read a ring ahead.  The max is a reference, the row's max when it last moved, rounded up, plus kMaskedKeep; it moves when a score passes it.
+// Nothing in an iteration but the masks is conditional: with the three parts behind conditions of their own the compiler held the accumulators twice, and spilled.
+//
+// RW = 4, KQ = 1: 128 rows.  RW = 2, KQ = 2: 64 rows and half as many steps, for fewer items than the units hold workgroups of the first kind (32 heads over 8, causal, d = 128,
+// N = 777 21.9 / 16.5 us, 1024 25.9 / 19.8, 1500 37.3 / 34; 2048, where they are as many, 50.7 / 56).
+//
+// What bounds it.  d = 128: the matrix unit has 512 cycles of a step and wave, the vector unit 413 (890 with a cap: two exponentials, a reciprocal and five
+// other instructions a score), and two waves share a SIMD: a step takes 850 (1140) cycles, at the 1.8 GHz that the power leaves.  Whether the fragments come a ring of 4 or
+// of 8 ahead, products in turn or one kind after the other, scheduled here or by the compiler, moves it by 1 %.  32 heads over 8, N = 8192, causal: 502 us, 1095 TFLOP/s (the
+// best kernel of Alg. 1 470, the baseline 506, a large matrix product 1256), with a cap 643.  d = 64: the vector unit, three waves a SIMD: 4 x 16 heads of 4096 166 us
+// (190 for Alg. 1 on that card), with a bias 182.
+// One after the other, tile by tile (K and V of 64 keys in two buffers, ascending, an exact max in each), the first form: 538 us, with a cap 666; d = 64 198, with a bias
+// 240; 32 heads, N = 777 21.6, with a cap 25.8.
 constexpr float kMaskedKeep = 8.f;
 
 struct MaskedParams {
@@ -67,7 +78,7 @@ struct Masked {
     static constexpr int S = KQ == 1 ? 4 : 2;          // slots of each
     static constexpr int LI = SLOT / 4096;             // load instructions of a wave and slot
     static constexpr bool AHEAD = S == 4;              // slots are there a step early, and a step's first fragments are read in the one before
-    static constexpr int R = D == 128 ? 8 : 4;  // fragments under way
+    static constexpr int R = D == 128 ? 8 : 4;         // fragments under way
     static constexpr int LDS_BYTES = 2 * S * SLOT;
     static_assert(RW * KQ == 4, "four waves");
     static_assert(KQ == 1 || 4 * (D * 64 + 256) <= LDS_BYTES, "the partial sums have to fit the slots' memory");
@@ -193,7 +204,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_masked_kernel(const
         auto first_key = [&](int s) { return (b_hi - 1 - s) * KT + 32 * kq; };  // of the wave
 
         // What a step's scores start from: a bias's part that is linear in the key's place, as one more product, of the places 0 .. 31 (exact in bf16) with the
-        // slope in three pieces of bf16.  (A multiply-add for each score instead: 4 x 16 heads of 4096, d = 64, 201 us, 1xx)
+        // slope in three pieces of bf16: sixteen multiply-adds of a step less.
         bf16x4 places, pieces;
         if (BIAS && !CAP) {
             float rest = lin;

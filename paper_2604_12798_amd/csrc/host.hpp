@@ -1,4 +1,4 @@
-// What the C entry points of both translation units (vfa_fwd.hip, serving.hip) use on the host.
+// What the C entry points of the translation units (vfa_fwd.hip, serving.hip, masked.hip) use on the host.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
