@@ -203,8 +203,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_masked_kernel(const
         auto whole = [&](int s) { return (uint32_t)(s - w_lo) < w_many; };
         auto first_key = [&](int s) { return (b_hi - 1 - s) * KT + 32 * kq; };  // of the wave
 
-        // What a step's scores start from: a bias's part that is linear in the key's place, as one more product, of the places 0 .. 31 (exact in bf16) with the
-        // slope in three pieces of bf16: sixteen multiply-adds of a step less.
+        // A bias's part that is linear in the key's place, as one more product, of the places 0 .. 31 (exact in bf16) with the slope in three pieces of bf16: sixteen
+        // multiply-adds of a step less.  It comes behind those of Q.K^T, which would be rounded at its size otherwise.
         bf16x4 places, pieces;
         if (BIAS && !CAP) {
             float rest = lin;
@@ -215,14 +215,14 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_masked_kernel(const
                 rest -= (float)pieces[e];
             }
         }
-        auto before = [&](bool on_left) __attribute__((always_inline)) -> f32x16 {
-            if (!BIAS || CAP) return f32x16{0};
+        auto slant = [&](const f32x16& st, bool on_left) __attribute__((always_inline)) -> f32x16 {
+            if (!BIAS || CAP) return st;
             u32x2 b = __builtin_bit_cast(u32x2, pieces);
             if (!on_left) {
                 b[0] ^= 0x80008000u;
                 b[1] ^= 0x80008000u;
             }
-            return __builtin_amdgcn_mfma_f32_32x32x8bf16_1k(__builtin_bit_cast(s16x4, places), __builtin_bit_cast(s16x4, b), f32x16{0}, 0, 0, 0);
+            return __builtin_amdgcn_mfma_f32_32x32x8bf16_1k(__builtin_bit_cast(s16x4, places), __builtin_bit_cast(s16x4, b), st, 0, 0, 0);
         };
         // the softmax of a step, in parts: pairs of scores to v (CAP), the max, pairs of v to weights
         float add = -INFINITY;  // A - the max
@@ -283,7 +283,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_masked_kernel(const
                     const int f = e >> 1;
                     ot[f % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[e % R], pf(po, f / DB), ot[f % DB], 0, 0, 0);
                 } else {
-                    sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[e % R], qf[e >> 1], e == 0 ? before(PLAIN || left(s + 1)) : sn, 0, 0, 0);
+                    sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[e % R], qf[e >> 1], e == 0 ? f32x16{0} : sn, 0, 0, 0);
+                    if (e == M - 2) sn = slant(sn, PLAIN || left(s + 1));
                 }
                 if (e + R < M) fr[e % R] = frag(e + R, slot_k, slot_v);
                 else if (F::AHEAD) fr[e % R] = frag(e + R - M, next_k, next_v);
@@ -373,9 +374,10 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_masked_kernel(const
 #pragma unroll
             for (int q = 0; q < 8; ++q) pa[q] = 0;
             iteration(s, S - 1, std::false_type{}, [&](uint32_t, uint32_t) __attribute__((always_inline)) {
-                sa = before(left(front));
+                sa = f32x16{0};
 #pragma unroll
                 for (int kk = 0; kk < KK; ++kk) sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_k(0, kk), qf[kk], sa, 0, 0, 0);
+                sa = slant(sa, left(front));
                 __builtin_amdgcn_sched_barrier(0);
                 if (F::AHEAD) {  // (of K of step front + 1, V of step front - 1)
 #pragma unroll

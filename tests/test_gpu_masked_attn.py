@@ -129,6 +129,16 @@ def test_any_ranges(vfa, d, bias):
             check(vfa, *prompt(1, 2, 4, 4, N, d), ranges=torch.tensor(r, dtype=torch.int32), causal=causal, slopes=SLOPES if bias else None)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+def test_steep_biases_on_short_documents(vfa, d, cap):
+    # the bias of a key's place in its block of 32 is far above the scores there
+    rng = random.Random(d)
+    for N in (5, 33, 44, 97, 600):
+        offsets = [documents(rng, N, 4) for _ in range(2)]
+        check(vfa, *prompt(N, 2, 4, 2, N, d, 0.1), ranges=ranges_of(offsets, None, N, True), cap=cap, slopes=[3.0, -2.7, 40.0, 0.9])
+
+
 @pytest.mark.parametrize("Hq,Hkv", [(1, 1), (8, 1), (6, 3), (16, 8), (9, 9)])
 def test_heads(vfa, Hq, Hkv):
     check(vfa, *prompt(Hq, 3, Hq, Hkv, 150, 128), slopes=[0.01 * h for h in range(Hq)])
