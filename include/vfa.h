@@ -406,8 +406,10 @@ int vfa_kv8_decode_fwd(const void* Q, const void* K8, const void* V8, const void
  * these calls sets a function attribute: each may be captured first.
  *
  * Scores.  s = softmax_scale * q . k (softmax_scale <= 0: 1 / sqrt(d)); with score_cap > 0 it becomes score_cap * tanh(s / score_cap); with slopes,
- * fp32 [Hq] on the device, slopes[h] * |distance between the positions of row and key| is subtracted from that.  score_cap is 0 (none) or 0.001 to 1000.
- * Scores and sums are held in fp32 (a cap's error is 2^-22 of it, which is an error of the exponents).
+ * fp32 [Hq] on the device, slopes[h] * |distance between the positions of row and key| is subtracted from that.  score_cap is 0 (none) or 0.001 to 1000,
+ * a given softmax_scale 2^-64 to 2^16 (else VFA_ERR_INVALID_ARG); scores, and a slope times the longest distance, are at most 2^28 in magnitude.  Scores and
+ * sums are held in fp32: a cap's error is 2^-22 of it, a bias's 2^-22 * slope * distance (in prompts distance + 56, for keys outside of the row's own
+ * block of 32), which are errors of the exponents.
  *
  * The cache is a pool of pages, KP, VP [n_pages, Hkv, page, d] bf16 (page a power of two, 16 or more, else VFA_ERR_UNSUPPORTED; 16-byte aligned),
  * and a table, int32 [B, max_pages] on the device: token n of sequence b lies in page table[b][n / page], row n % page.  max_pages * page <= 2^30.  An

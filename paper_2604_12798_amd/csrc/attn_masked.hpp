@@ -13,7 +13,8 @@ namespace {
 //
 // A score's log2 weight is A + F v.  Without a cap v is what the matrix unit gives and F = c; with one v = 1 / (1 + e^(2 s / cap)), F = -2 cap2 and A = cap2 (see
 // Scores).  A bias -slope |i - j| is linear in the key's place in the step on either side of the row: that part goes into v, and the rest is the
-// step's A.
+// step's A, so that up to 62 slopes are rounded and cancel.  Of the step across the rows, the one with the nearest keys, the distances are taken one by one: they go into v, and
+// A is 0.
 //
 // Iteration s of a wave: Q.K^T of its step s + 1 and P.V of its step s - 1, a product of each in turn, with the softmax of step s dealt out between them, and the
 // fragments of the products read a ring ahead.  The max is a reference, the row's max when it last moved, rounded up, plus kMaskedKeep; it moves when a score passes it.
@@ -70,6 +71,8 @@ __device__ __forceinline__ void request1_at(const u32x4& rsrc, uint32_t at, uint
                  : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(o0), "s"(rsrc), "s"(__builtin_amdgcn_readfirstlane(at))
                  : "memory", "m0");
 }
+
+enum class Side { left, across, right };  // of a wave's keys of a step: all at or before its rows, both, all at or behind them
 
 template <int D, int RW, int KQ>
 struct Masked {
@@ -198,8 +201,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_masked_kernel(const
         const int w_lo = b_hi - (all_hi >= 32 * kq + 32 ? (all_hi - 32 * kq - 32) / KT + 1 : 0), w_hi = b_hi - (max(all_lo - 32 * kq, 0) + KT - 1) / KT;
         const int f_lo = b_hi - wg_all_hi / KT, f_hi = b_hi - (wg_all_lo + KT - 1) / KT;
         const uint32_t w_many = max(w_hi - w_lo, 0), f_many = max(f_hi - f_lo, 0);
-        auto left = [&](int s) { return !BIAS || s >= l_lo; };
-        auto right = [&](int s) { return s < r_hi; };
+        auto side_of = [&](int s) { return !BIAS || s >= l_lo ? Side::left : s < r_hi ? Side::right : Side::across; };
         auto whole = [&](int s) { return (uint32_t)(s - w_lo) < w_many; };
         auto first_key = [&](int s) { return (b_hi - 1 - s) * KT + 32 * kq; };  // of the wave
 
@@ -215,37 +217,35 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_masked_kernel(const
                 rest -= (float)pieces[e];
             }
         }
-        auto slant = [&](const f32x16& st, bool on_left) __attribute__((always_inline)) -> f32x16 {
+        auto slant = [&](const f32x16& st, Side side) __attribute__((always_inline)) -> f32x16 {
             if (!BIAS || CAP) return st;
             u32x2 b = __builtin_bit_cast(u32x2, pieces);
-            if (!on_left) {
-                b[0] ^= 0x80008000u;
-                b[1] ^= 0x80008000u;
-            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) b[e] = side == Side::left ? b[e] : side == Side::right ? b[e] ^ 0x80008000u : 0u;
             return __builtin_amdgcn_mfma_f32_32x32x8bf16_1k(__builtin_bit_cast(s16x4, places), __builtin_bit_cast(s16x4, b), st, 0, 0, 0);
         };
         // the softmax of a step, in parts: pairs of scores to v (CAP), the max, pairs of v to weights
         float add = -INFINITY;  // A - the max
-        auto offset = [&](int s, bool on_left) __attribute__((always_inline)) {  // A
+        auto offset = [&](int s, Side side) __attribute__((always_inline)) {  // A
             const int away = qrow - first_key(s) - (CAP ? 4 * hh : 0);
-            const float base = BIAS ? slope2 * (float)(on_left ? -away : away) : 0.f;
+            const float base = BIAS ? (side == Side::left ? -slope2 : side == Side::right ? slope2 : 0.f) * (float)away : 0.f;
             return CAP ? P.s.cap2 + base : base;
         };
-        auto part_a = [&](f32x16& st, bool on_left, int q) __attribute__((always_inline)) {
+        auto part_a = [&](f32x16& st, Side side, int q) __attribute__((always_inline)) {
 #pragma unroll
             for (int e = 2 * q; e < 2 * q + 2; ++e) {
                 st[e] = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(st[e] * P.s.capk));
-                if (BIAS) st[e] = __builtin_fmaf(on_left ? lin : -lin, (float)(8 * (e >> 2) + (e & 3)), st[e]);
+                if (BIAS) st[e] = __builtin_fmaf(side == Side::left ? lin : side == Side::right ? -lin : 0.f, (float)(8 * (e >> 2) + (e & 3)), st[e]);
             }
         };
         // Products of po that have been started are in ot, those to come take the changed po: the max may move between any two of them.  It moves by whole
         // numbers, so that weights in bf16 are rescaled exactly.  (Each row by itself: what the others see changes none of its bits.)
-        auto part_m = [&](const f32x16& st, uint32_t* po, int s, bool on_left) __attribute__((always_inline)) {
+        auto part_m = [&](const f32x16& st, uint32_t* po, int s, Side side) __attribute__((always_inline)) {
             float x = st[0];
 #pragma unroll
             for (int q = 0; q < 7; ++q) x = CAP ? fminf(fminf(x, st[1 + 2 * q]), st[2 + 2 * q]) : fmaxf(fmaxf(x, st[1 + 2 * q]), st[2 + 2 * q]);
             x = CAP ? fminf(x, st[15]) : fmaxf(x, st[15]);
-            const float a = offset(s, on_left), y = __builtin_fmaf(x, fac, a);  // (with a cap and a bias A differs between the halves)
+            const float a = offset(s, side), y = __builtin_fmaf(x, fac, a);  // (with a cap and a bias A differs between the halves)
             const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
             const float top = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
             if (__builtin_expect(__builtin_amdgcn_ballot_w64(top > m2) != 0, 0)) {
@@ -284,7 +284,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_masked_kernel(const
                     ot[f % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[e % R], pf(po, f / DB), ot[f % DB], 0, 0, 0);
                 } else {
                     sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[e % R], qf[e >> 1], e == 0 ? f32x16{0} : sn, 0, 0, 0);
-                    if (e == M - 2) sn = slant(sn, PLAIN || left(s + 1));
+                    if (e == M - 2) sn = slant(sn, PLAIN ? Side::left : side_of(s + 1));
                 }
                 if (e + R < M) fr[e % R] = frag(e + R, slot_k, slot_v);
                 else if (F::AHEAD) fr[e % R] = frag(e + R - M, next_k, next_v);
@@ -298,13 +298,13 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_masked_kernel(const
 #pragma unroll
             for (int e = 0; e < H; ++e) {
 #pragma unroll
-                for (int u = 8 * e / H; u < 8 * (e + 1) / H; ++u) part_a(st, PLAIN || left(s), u);
+                for (int u = 8 * e / H; u < 8 * (e + 1) / H; ++u) part_a(st, PLAIN ? Side::left : side_of(s), u);
                 product(e);
             }
             const int key0 = first_key(s) + 4 * hh;
-            if (BIAS && !PLAIN && !left(s) && !right(s)) {  // (part_a counts the distance as if on the right)
+            if (BIAS && !PLAIN && side_of(s) == Side::across) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) st[r] = __builtin_fmaf(-2.f * lin, fmaxf((float)(qrow - key0 - 8 * (r >> 2) - (r & 3)), 0.f), st[r]);
+                for (int r = 0; r < 16; ++r) st[r] = __builtin_fmaf(-lin, __builtin_fabsf((float)(qrow - key0 - 8 * (r >> 2) - (r & 3))), st[r]);
             }
             if (!PLAIN && !whole(s)) {
                 const uint32_t first = own.x - key0, many = own.y - own.x;
@@ -316,7 +316,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_masked_kernel(const
             for (int e = H; e < M; ++e) {
 #pragma unroll
                 for (int u = 10 * (e - H) / (M - H); u < 10 * (e - H + 1) / (M - H); ++u) {
-                    if (u == 0) part_m(st, po, s, PLAIN || left(s));
+                    if (u == 0) part_m(st, po, s, PLAIN ? Side::left : side_of(s));
                     else if (u >= 2) part_b(st, pk, u - 2);
                 }
                 product(e);
@@ -377,7 +377,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_masked_kernel(const
                 sa = f32x16{0};
 #pragma unroll
                 for (int kk = 0; kk < KK; ++kk) sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_k(0, kk), qf[kk], sa, 0, 0, 0);
-                sa = slant(sa, left(front));
+                sa = slant(sa, side_of(front));
                 __builtin_amdgcn_sched_barrier(0);
                 if (F::AHEAD) {  // (of K of step front + 1, V of step front - 1)
 #pragma unroll

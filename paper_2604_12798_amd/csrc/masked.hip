@@ -42,6 +42,9 @@ bool whole_runs(long long a, long long b, long long c) { return ((a | b | c) & 7
 
 // cap: 0 = none, else 0.001 to 1000 (see Scores)
 bool cap_ok(float cap) { return cap == 0.f || (cap >= 0.001f && cap <= 1000.f); }
+// A slope over the least stays far from the end of fp32; with more than the largest, scores of ordinary rows pass 2^28, where the difference to a rounded max
+// may be an exponent that gives infinity
+bool scale_ok(float scale) { return scale <= 0.f || (scale >= 0x1p-64f && scale <= 0x1p16f); }
 Scores scores_of(const float* slopes, float cap, float scale) { return Scores{slopes, cap * kLog2e, cap > 0.f ? 2.f * kLog2e * scale / cap : 0.f}; }
 
 template <typename F>
@@ -118,7 +121,7 @@ int vfa_kvp_decode_fwd(const void* Q, const void* KP, const void* VP, const int*
     const int rc = check_pages(KP, VP, n_pages, table, max_pages, B, Hkv, page, d, &done);
     if (rc != VFA_OK) return rc;
     const int n_cap = max_pages * page;
-    if (Hq <= 0 || Hq % Hkv != 0 || n_q < 0 || n_splits < 1 || n_splits > 4096 || !isfinite(softmax_scale) || !cap_ok(score_cap)) return VFA_ERR_INVALID_ARG;
+    if (Hq <= 0 || Hq % Hkv != 0 || n_q < 0 || n_splits < 1 || n_splits > 4096 || !isfinite(softmax_scale) || !scale_ok(softmax_scale) || !cap_ok(score_cap)) return VFA_ERR_INVALID_ARG;
     if (!aligned4(seq_lens) || !aligned4(slopes) || (!seq_lens && (n_keys < 0 || n_keys > n_cap))) return VFA_ERR_INVALID_ARG;
     const int g = Hq / Hkv;
     if (g > 32) return VFA_ERR_UNSUPPORTED;
@@ -193,7 +196,7 @@ int vfa_row_ranges(const int* doc_offsets, const int* prefix_lens, int* ranges, 
 int vfa_masked_attn_fwd(const void* Q, const void* K, const void* V, void* O, float* LSE, int B, int Hq, int Hkv, int N, int d, int causal,
                         const int* ranges, float softmax_scale, float score_cap, const float* slopes, void* stream) {
     if (B < 0 || Hq <= 0 || Hkv <= 0 || N < 0 || d <= 0 || Hq % Hkv != 0 || (causal != 0 && causal != 1)) return VFA_ERR_INVALID_ARG;
-    if (!isfinite(softmax_scale) || !cap_ok(score_cap)) return VFA_ERR_INVALID_ARG;
+    if (!isfinite(softmax_scale) || !scale_ok(softmax_scale) || !cap_ok(score_cap)) return VFA_ERR_INVALID_ARG;
     if (d != 64 && d != 128) return VFA_ERR_UNSUPPORTED;
     if (!aligned8(ranges) || !aligned4(slopes) || !aligned4(LSE)) return VFA_ERR_INVALID_ARG;
     if (B == 0 || N == 0) return VFA_OK;

@@ -16,8 +16,7 @@ def attend(q, k, v, seen, away, cap, slope, scale=None, weights=HALF_BF16):
     sum, a reciprocal of 1 ulp and a multiply-add, 2^-21 of the cap is above their sum; an error of the score goes through it at most once.  A bias by the distance rounds the
     slope times log2(e), the distance, their product and the sum: four roundings of slope * distance.  A kernel may take it in two parts, slope times the key's place in a block
     of 32 keys, in units of raw scores, and slope times the rest, which then are up to slope * 31 and slope * (distance + 31).  The first rounds the slope over the scale, the slope in
-    pieces and three products' sums (5 * 31); where rows and keys of a block cross, twice the distance is taken off it, of up to 62: that slope's rounding and the sum's (4 * 31).  The
-    rest rounds its product and its difference to the max (2 * 31 beside the distance's own).  Together slope * (4 * distance + 11 * 32) at most.
+    pieces and three products' sums (5 * 31), the rest its product and its difference to the max (2 * 31 beside the distance's own): slope * (4 * distance + 7 * 32) at most.
     The exponent's own product with log2(e) and the difference to the max round
     at the scores' magnitude, four more.  An error of e of all exponents changes a weight by e and the sum that divides by at most e: 2 e (1 % is far above the
     second order).  The row's sums have at most m terms: 2 m roundings.  `weights`: the rounding of weights for the product with V.  Then one rounding of the output."""
@@ -32,7 +31,7 @@ def attend(q, k, v, seen, away, cap, slope, scale=None, weights=HALF_BF16):
         err = err + 2.0 ** -21 * cap
     if slope is not None:
         x = x - slope * away
-        err = err + HALF_F32 * abs(slope) * (4 * away + 11 * 32)
+        err = err + HALF_F32 * abs(slope) * (4 * away + 7 * 32)
     err = err + 4 * HALF_F32 * torch.nan_to_num(x, nan=0.0, posinf=0.0, neginf=0.0).abs()
     err = torch.where(seen, err, 0).amax(-1, keepdim=True) if k.shape[0] else torch.zeros((q.shape[0], 1), dtype=F64)
     x = torch.where(seen, x, -math.inf)

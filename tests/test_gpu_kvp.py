@@ -163,6 +163,9 @@ def test_decode_scores(vfa, d, cap, bias, n_q, n_splits):
 def test_decode_scale(vfa):
     check_decode(vfa, gen(3), [100, 200], 8, 2, 64, 16, cap=20.0, slopes=SLOPES, scale=0.3)
     check_decode(vfa, gen(3), [100, 200], 8, 2, 64, 16, scale=0.01)
+    for cap in (0.0, 1.0):
+        check_decode(vfa, gen(3), [100, 200], 8, 2, 64, 16, cap=cap, slopes=SLOPES[:7] + [2.0 ** 20], scale=2.0 ** -64)
+        check_decode(vfa, gen(3), [100, 200], 8, 2, 64, 16, cap=cap, slopes=SLOPES, scale=2.0 ** 16)
 
 
 @pytest.mark.parametrize("d", [64, 128])

@@ -150,6 +150,15 @@ def test_scale(vfa):
 
 
 @pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("cap", [0.0, 1.0])
+def test_scales_and_slopes_at_the_ends(vfa, d, cap):
+    for N in (40, 500):
+        check(vfa, *prompt(7, 1, 2, 1, N, d), scale=2.0 ** -64, cap=cap, slopes=[0.3, 2.0 ** 18])
+        check(vfa, *prompt(7, 1, 2, 1, N, d), scale=2.0 ** -64, cap=cap, slopes=[-(2.0 ** 18), 2.0 ** 12], causal=False)
+        check(vfa, *prompt(7, 1, 2, 1, N, d), scale=2.0 ** 16, cap=cap, slopes=[0.3, 0.0])
+
+
+@pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("cap,bias", SCORES)
 def test_long(vfa, d, cap, bias):
     """Rows of a longer prompt: first, last and some between."""

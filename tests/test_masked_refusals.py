@@ -109,6 +109,17 @@ def test_masked(p):
         assert call(f, good, O=P, **bad) == UNSUPPORTED, bad
 
 
+def test_scales_out_of_range(p):
+    decode = dict(Q=P, KP=P, VP=P, table=P, O=NONE, LSE=NONE, B=0, Hq=4, Hkv=2, n_pages=9, page=16, M=8, n_q=1, d=64, lens=NONE, n_keys=4, ns=1, scale=0.0, cap=0.0,
+                  slopes=NONE, ws=NONE, wsb=0, stream=NONE)
+    prompt = dict(Q=P, K=P, V=P, O=NONE, LSE=NONE, B=0, Hq=4, Hkv=2, N=4, d=64, causal=1, ranges=NONE, scale=0.0, cap=0.0, slopes=NONE, stream=NONE)
+    for f, good in ((p.lib().vfa_kvp_decode_fwd, decode), (p.lib().vfa_masked_attn_fwd, prompt)):
+        for scale in (2.0 ** -65, 1e-40, 2.0 ** 17, 2.0 ** 64, 3e38):
+            assert call(f, good, scale=scale) == INVALID, scale
+        for scale in (2.0 ** -64, 2.0 ** 16, -1.0, -3e38):
+            assert call(f, good, scale=scale) == OK, scale
+
+
 def test_numbers_past_the_range_of_their_type(p):
     """No sequences, so that nothing is launched: a number that its C type does not hold is refused, and not taken by its low bits."""
     n = p._ns()
