@@ -19,7 +19,8 @@ def attend(q, k, v, seen, away, cap, slope, scale=None, weights=HALF_BF16):
     pieces and three products' sums (5 * 31), the rest its product and its difference to the max (2 * 31 beside the distance's own): slope * (4 * distance + 7 * 32) at most.
     The exponent's own product with log2(e) and the difference to the max round
     at the scores' magnitude, four more.  An error of e of all exponents changes a weight by e and the sum that divides by at most e: 2 e (1 % is far above the
-    second order).  The row's sums have at most m terms: 2 m roundings.  `weights`: the rounding of weights for the product with V.  Then one rounding of the output."""
+    second order).  The row's sums have at most m terms: 2 m roundings.  `weights`: the rounding of weights for the product with V (twice where
+    the max moves between them and the product, but then they are 2^-8 of the new max at most, and 2^-16 is less than 1 % of 2^-8).  Then one rounding of the output."""
     q, k, v = q.to(F64), k.to(F64), v.to(F64)
     scale = q.shape[1] ** -0.5 if scale is None else scale
     x = q @ k.T * scale

@@ -144,6 +144,19 @@ def test_heads(vfa, Hq, Hkv):
     check(vfa, *prompt(Hq, 3, Hq, Hkv, 150, 128), slopes=[0.01 * h for h in range(Hq)])
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("cap,bias", SCORES)
+@pytest.mark.parametrize("N", [1, 40, 333])
+def test_rows_that_see_one_key_get_its_value(vfa, d, cap, bias, N):
+    # its weight is a power of two and the sum that weight within 2^-16, far below half a step of bf16
+    Q, K, V = (x.cuda() for x in prompt(N, 2, 4, 2, N, d))
+    key = torch.randint(0, N, (2, N), generator=torch.Generator().manual_seed(N)).int()
+    slopes = torch.tensor(SLOPES, device="cuda") if bias else None
+    O, _ = vfa.masked_attn_fwd(Q, K, V, causal=False, ranges=torch.stack((key, key + 1), -1).cuda(), score_cap=cap, slopes=slopes)
+    at = key.cuda().long()[:, None, :, None].expand(2, 4, N, d)
+    assert torch.equal(O, V.repeat_interleave(2, 1).gather(2, at))
+
+
 def test_scale(vfa):
     check(vfa, *prompt(7, 1, 2, 1, 100, 64), scale=0.4, cap=10.0, slopes=[0.1, 0.0])
     check(vfa, *prompt(7, 1, 2, 1, 100, 64), scale=0.02)
