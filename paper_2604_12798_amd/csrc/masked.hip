@@ -151,7 +151,9 @@ int vfa_kvp_decode_fwd(const void* Q, const void* KP, const void* VP, const int*
     hipStream_t s = (hipStream_t)stream;
     const int n_cu = cu_count() > 0 ? cu_count() : 256;
     (void)hipGetLastError();
-    const bool dealt = seq_lens && n_splits > 1 && B > 1 && (B <= 64 || (B <= DEAL_MAX_B && (long long)B * Hkv * n_splits <= 8LL * n_cu && ceil_div(n_cap, BN) > 2 * n_splits));
+    // (dealing counts the batch's tiles in an int: pages may be shared or missing, so the memory that the tokens would take does not bound them)
+    const bool countable = (long long)B * (ceil_div(n_cap, BN) + n_splits) <= 0x7fffffffLL;
+    const bool dealt = countable && seq_lens && n_splits > 1 && B > 1 && (B <= 64 || (B <= DEAL_MAX_B && (long long)B * Hkv * n_splits <= 8LL * n_cu && ceil_div(n_cap, BN) > 2 * n_splits));
     with_d(d, [&](auto d_c) {
         constexpr int D = decltype(d_c)::value;
         // (dealt out, there are enough ranges for one wave each)

@@ -1,0 +1,36 @@
+"""Which kernels the paged cache and masked attention launch, and with what.  CPU only: the launches are written down, not made."""
+import os
+import struct
+
+import pytest
+
+import launch_util
+from launch_util import P
+from paper_2604_12798_amd import build
+
+NULL = 0
+
+
+@pytest.fixture(scope="module")
+def launches(tmp_path_factory):
+    if not os.path.exists(build.LIB) or not os.path.exists(build.BINDING):
+        build.build_lib()
+    log = launch_util.build(tmp_path_factory.mktemp("launches"))
+    return lambda calls: launch_util.launches(log, calls)
+
+
+ONE, FIXED, DEALT = 0, 1, 2  # what the lengths of a decode's sequences are to its kernel (its third template argument)
+
+
+def decode(B, Hq, Hkv, page, M, n_splits, n_q=1, d=64, lens=P, n_keys=0):
+    return ("vfa_kvp_decode_fwd", [P, P, P, P, P, P, B, Hq, Hkv, 9, page, M, n_q, d, lens, n_keys, n_splits, 0.0, 0.0, NULL, P, 1 << 40, NULL], 0)
+
+
+def test_ranges_are_dealt_only_where_an_int_counts_the_tiles(launches):
+    """Sequences may share pages or miss them, so 128 of 2^30 tokens are a call like others: 2^31 tiles, which an int does not hold.  The search of a range's sequence would
+    end at once, all ranges would be those of the first one, and the merge would read entries of the others that nobody wrote."""
+    page, M = 1 << 14, 1 << 16
+    calls = [decode(B, 1, 1, page, M, 2) for B in (2, 64, 127, 128, 200)] + [decode(64, 1, 1, page, M, 4096), decode(100, 1, 1, page, M // 2, 2)]
+    for (rc, made), form in zip(launches(calls), (DEALT, DEALT, DEALT, FIXED, FIXED, DEALT, DEALT)):
+        assert rc == 0 and [m[0] for m in made] == ["kvp_decode_kernel", "decode_merge_kernel"]
+        assert made[0][1][2] == form and made[1][1][1] == (2 if form == DEALT else 0)
