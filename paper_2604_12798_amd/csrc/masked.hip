@@ -189,6 +189,7 @@ int vfa_row_ranges(const int* doc_offsets, const int* prefix_lens, int* ranges, 
     if (!doc_offsets || !ranges) return VFA_ERR_INVALID_ARG;
     const long long groups = ((long long)N + 255) / 256;
     if (B > 65535 || n_docs == 0x7fffffff || groups * B > kMaxWorkgroups256) return VFA_ERR_UNSUPPORTED;
+    if (!causal) prefix_lens = nullptr;  // (not read: all of a document is seen as it is)
     const RowRanges p{doc_offsets, prefix_lens, reinterpret_cast<int2*>(ranges), N, n_docs, causal};
     (void)hipGetLastError();
     row_ranges_kernel<<<dim3((unsigned)groups, (unsigned)B), 256, 0, (hipStream_t)stream>>>(p);

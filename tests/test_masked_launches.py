@@ -34,3 +34,11 @@ def test_ranges_are_dealt_only_where_an_int_counts_the_tiles(launches):
     for (rc, made), form in zip(launches(calls), (DEALT, DEALT, DEALT, FIXED, FIXED, DEALT, DEALT)):
         assert rc == 0 and [m[0] for m in made] == ["kvp_decode_kernel", "decode_merge_kernel"]
         assert made[0][1][2] == form and made[1][1][1] == (2 if form == DEALT else 0)
+
+
+def test_prefixes_are_read_for_causal_documents_only(launches):
+    """The header says that prefix_lens is not read for causal = 0, so it may be anything there."""
+    made = launches([("vfa_row_ranges", [P, 2 * P, 3 * P, 1, 1000, 2, causal, NULL], 24) for causal in (1, 0)])
+    for (rc, [kernel]), prefix in zip(made, (2 * P, 0)):
+        assert rc == 0 and kernel[0] == "row_ranges_kernel" and kernel[2] == (4, 1, 1)
+        assert struct.unpack("<3Q", kernel[4]) == (P, prefix, 3 * P)
