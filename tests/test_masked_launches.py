@@ -42,3 +42,23 @@ def test_prefixes_are_read_for_causal_documents_only(launches):
     for (rc, [kernel]), prefix in zip(made, (2 * P, 0)):
         assert rc == 0 and kernel[0] == "row_ranges_kernel" and kernel[2] == (4, 1, 1)
         assert struct.unpack("<3Q", kernel[4]) == (P, prefix, 3 * P)
+
+
+def prompt(B, Hq, Hkv, N, d, cap=0.0, slopes=NULL):
+    return ("vfa_masked_attn_fwd", [P, P, P, P, P, B, Hq, Hkv, N, d, 1, P, 0.0, cap, slopes, NULL], 0)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_rows_of_a_workgroup_of_masked_attention(launches, d):
+    """128 where the units (256 without a GPU) hold no more workgroups of them than there are, two of them each, three at d = 64; else 64.  All kinds of scores."""
+    places = 512 if d == 128 else 768
+    calls, want = [], []
+    for items, blocks in ((places, 1), (places - 1, 1), (places, 4), (places - 4, 4), (5 * places, 5), (1, 1)):
+        for cap, slopes in ((0.0, NULL), (30.0, NULL), (0.0, P), (50.0, P)):
+            for N in (128 * blocks, 128 * blocks - 127):
+                calls.append(prompt(1, items // blocks, 1, N, d, cap, slopes))
+                many = items >= places
+                want.append(((d, 4, 1) if many else (d, 2, 2)) + (int(cap > 0), int(slopes != NULL)) + (items // blocks * -(-N // (128 if many else 64)),))
+    for (rc, made), w in zip(launches(calls), want):
+        [(name, form, grid, block, _)] = made
+        assert rc == 0 and name == "attn_masked_kernel" and form == w[:5] and grid == (w[5], 1, 1) and block == (256, 1, 1)
