@@ -47,6 +47,15 @@ bool cap_ok(float cap) { return cap == 0.f || (cap >= 0.001f && cap <= 1000.f); 
 bool scale_ok(float scale) { return scale <= 0.f || (scale >= 0x1p-64f && scale <= 0x1p16f); }
 Scores scores_of(const float* slopes, float cap, float scale) { return Scores{slopes, cap * kLog2e, cap > 0.f ? 2.f * kLog2e * scale / cap : 0.f}; }
 
+// Whether the ranges of a batch of sequences of up to `tiles` tiles are dealt out by length (see varlen_find, which also says why not): they are counted in an int, and pages may be
+// shared or missing, so that the memory that tokens would take does not bound them.
+constexpr int DEAL_FREELY_B = 64;
+constexpr long long kDealtPerUnit = 8;
+bool deals(int B, int Hkv, int n_splits, int tiles, int n_cu) {
+    if (n_splits <= 1 || B <= 1 || (long long)B * ((long long)tiles + n_splits) > 0x7fffffffLL) return false;
+    return B <= DEAL_FREELY_B || (B <= DEAL_MAX_B && (long long)B * Hkv * n_splits <= kDealtPerUnit * n_cu && tiles > 2 * n_splits);
+}
+
 template <typename F>
 void with_d(int d, F f) {
     if (d == 128) f(std::integral_constant<int, 128>{});
@@ -92,9 +101,17 @@ int vfa_kvp_append(const void* K, const void* V, void* KP, void* VP, const int* 
 
 // Two tiles a range at least (8 heads of 2048 keys, d = 128: 8 ranges 10.3 us, 16 9.4; of 600 1 12.1, 3 9.9, 4 9.8), one range where there are few.  Equal lengths:
 // as many ranges as compute units, whose workgroups of four waves have a unit each at d = 128 and half of one at d = 64 (32 heads of 32768 keys 4 ranges 96, 6 83, 8
-// 85, 16 87, 32 92; 128 of 4096: 1 55, 2 46, 4 50; 256 of 1000: 1 25.8, 2 30.6; 8 of 8000: 16 14.1, 32 11.8, 48 17.1; d = 64: 16 of 2048 8 8.7, 16 8.1).
+// 85, 16 87, 32 92; 128 of 4096: 1 55, 2 46, 4 50; 256 of 1000: 1 25.8, 2 30.6; 8 of 8000: 16 14.1, 32 11.8, 48 17.1; d = 64: 16 of 2048 8 8.7, 16 8.1).  Rounded down: 136 heads
+// of 1024 keys 1 range 17, 2 25, of 4096 52 / 68 (3: 53), of 16384 198 / 233 (3: 179); 192 of them 20 / 27, 66 / 75, 249 / 252; 248 of them 23 / 30, 83 / 88, 325 / 315.
 // Lengths of their own, dealt out to workgroups of one wave: as many as the units hold (128 heads of 200 to 8192 keys, d = 128: 4 ranges 55, 6 51, 8 49.5, 12 55, 16 56; with
-// four waves each 2 55, 4 54.6, 8 64.5; 64 of 500 to 16384: 8 49.9, 16 48.4, 24 55.8; d = 64, 128 of 300 to 8192: 8 28, 16 26.9, 24 29.6).
+// four waves each 2 55, 4 54.6, 8 64.5; 64 of 500 to 16384: 8 49.9, 16 48.4, 24 55.8; d = 64, 128 of 300 to 8192: 8 28, 16 26.9, 24 29.6), and above 64 sequences as many as are
+// dealt at all (100 heads of 1000 keys 7 ranges 16.8 dealt, 8 27 of four waves each; 80 of 1500 11 17.4, 12 28).
+// More than one and a half heads for each unit keep them busy with one range each if lengths are even, and wait for the longest if they are not.  Which they are is not known here, the
+// capacity is.  Even from 200 up to it / one of it and the others 200, 64 x 8 heads, d = 128: of 2048 1 range 48 / 33, 2 56 / 21, 4 58 / 24; of 4096 86 / 51, 97 / 21, 94 / 24; of 8192 166 / 87,
+// 182 / 23, 175 / 27; of 16384 324 / 160, 349 / 28, 341 / 34 (of 8192 50 x 8 136 / 86, 162 / 22, 145 / 25; 70 x 8 199 / 92, 209 / 25, three 203 / 28, four, not dealt, 199 / 68; d = 64, 64 x 8
+// 94 / 50, 97 / 16, 92 / 16).  So one up to 4096 keys, which one unit reads in 40 us (20 at d = 64), above that up to four while they are dealt.
+// More than 256 sequences are not dealt, but take more than one range above 2048 keys too (300 heads of 100 to 1000 keys 1 range 18, 3 31; of 4000 58 / 63, all of 4000 121 / 108; one of
+// 32768 and the others 200 288 / 115; 512 of 200 to 8192 168, 2 173, one of 8192 and the others 200 84 / 61).
 int vfa_kvp_decode_splits(int B, int Hq, int Hkv, int n_q, int d, int n_keys, int varlen) {
     if (B <= 0 || Hq <= 0 || Hkv <= 0 || n_q <= 0 || n_keys <= 0 || (long long)B * Hkv > 65535) return 1;
     const int n_cu = cu_count() > 0 ? cu_count() : 256, all = n_keys / BN + (n_keys % BN != 0);  // (n_keys + 63 may not fit)
@@ -102,10 +119,15 @@ int vfa_kvp_decode_splits(int B, int Hq, int Hkv, int n_q, int d, int n_keys, in
     const int g = Hq / Hkv, tokens = rows <= 32 ? n_q : g < 32 ? 32 / g : 1;
     const long long heads = (long long)B * Hkv * (((long long)n_q + tokens - 1) / tokens);  // (with more than 32 rows, groups of them)
     if (all <= (d == 64 ? 8 : 5)) return 1;
-    const bool dealt = varlen && B > 1 && rows <= 32;
-    const long long slots = (long long)n_cu * (d == 64 ? 2 : 1) * (dealt ? 4 : 1);
-    if (dealt && 2 * heads > 3LL * n_cu) return 1;  // (512 heads of 200 to 2048 keys: 1 range of four waves 53.1, 2 of one 55.8)
-    return (int)max(1LL, min(slots / heads, min((all + 1LL) / 2, 4096LL)));
+    const long long units = (long long)n_cu * (d == 64 ? 2 : 1);
+    auto bounded = [&](long long n) { return (int)max(1LL, min(n, min((all + 1LL) / 2, 4096LL))); };
+    if (!varlen || B == 1 || rows > 32) return bounded(units / heads);
+    const bool busy = 2 * heads > 3LL * n_cu;
+    if (busy && all <= 4096 / BN) return 1;
+    const int n = bounded(max(4 * units / heads, busy ? min(4LL, kDealtPerUnit * n_cu / heads) : 1));
+    const int dealt = B <= DEAL_FREELY_B ? n : (int)min((long long)n, min(kDealtPerUnit * n_cu / heads, (all - 1LL) / 2));
+    if (deals(B, Hkv, dealt, all, n_cu)) return dealt;
+    return bounded((all > 2048 / BN ? 4 : 1) * units / heads);
 }
 
 size_t vfa_kvp_decode_workspace_bytes(int B, int Hq, int n_q, int d, int n_splits) {
@@ -151,9 +173,7 @@ int vfa_kvp_decode_fwd(const void* Q, const void* KP, const void* VP, const int*
     hipStream_t s = (hipStream_t)stream;
     const int n_cu = cu_count() > 0 ? cu_count() : 256;
     (void)hipGetLastError();
-    // (dealing counts the batch's tiles in an int: pages may be shared or missing, so the memory that the tokens would take does not bound them)
-    const bool countable = (long long)B * (ceil_div(n_cap, BN) + n_splits) <= 0x7fffffffLL;
-    const bool dealt = countable && seq_lens && n_splits > 1 && B > 1 && (B <= 64 || (B <= DEAL_MAX_B && (long long)B * Hkv * n_splits <= 8LL * n_cu && ceil_div(n_cap, BN) > 2 * n_splits));
+    const bool dealt = seq_lens && deals(B, Hkv, n_splits, ceil_div(n_cap, BN), n_cu);
     with_d(d, [&](auto d_c) {
         constexpr int D = decltype(d_c)::value;
         // (dealt out, there are enough ranges for one wave each)

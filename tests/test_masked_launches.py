@@ -44,6 +44,41 @@ def test_prefixes_are_read_for_causal_documents_only(launches):
         assert struct.unpack("<3Q", kernel[4]) == (P, prefix, 3 * P)
 
 
+def test_suggested_ranges_are_of_the_form_that_they_are_counted_for(launches):
+    """Ranges of lengths on the GPU are counted for workgroups of one wave where they are dealt out, and so they are; else for workgroups of four waves."""
+    import paper_2604_12798_amd as vfa
+    calls, said = [], []
+    for d in (64, 128):
+        for Hkv in (1, 2, 8):
+            for B in (2, 17, 50, 63, 64, 65, 80, 100, 129, 200, 256, 257, 300):
+                for n in (400, 520, 1000, 1500, 2048, 2049, 4096, 4097, 32768):
+                    s = vfa.kvp_decode_splits(B, 4 * Hkv, Hkv, 1, d, n, True)
+                    said.append((d, Hkv, B, n, s))
+                    calls.append(decode(B, 4 * Hkv, Hkv, 16, -(-n // 16), s, d=d))
+    for (d, Hkv, B, n, s), (rc, made) in zip(said, launches(calls)):
+        assert rc == 0, (d, Hkv, B, n, s)
+        four_waves = max(1, 256 * (2 if d == 64 else 1) // (B * Hkv))
+        form = made[0][1][2]
+        if B <= 256:
+            assert (form == DEALT) == (s > 1), (d, Hkv, B, n, s)
+        elif n <= 2048:
+            assert form == FIXED and s <= four_waves, (d, Hkv, B, n, s)
+
+
+def test_a_long_sequence_among_many_gets_ranges():
+    """Many sequences keep the units busy with one range each, if none of them can be long; else the longest one would have a unit for each of its heads and no more."""
+    import paper_2604_12798_amd as vfa
+    s = lambda B, n, d=128, Hkv=8: vfa.kvp_decode_splits(B, 4 * Hkv, Hkv, 1, d, n, True)
+    for d in (64, 128):
+        assert s(64, 4096, d) == 1 and s(128, 1024, d) == 1
+        for n in (4097, 8192, 32768):
+            assert 2 <= s(64, n, d) <= 4 and s(128, n, d) == 2
+        assert s(256, 32768, d) == 1  # (2048 heads: not dealt with more)
+        assert 2 <= s(300, 32768, d, 1) and s(300, 1000, d, 1) == 1
+    assert s(100, 1000, 128, 1) == 7 and s(80, 1500, 128, 1) == 11
+    assert s(16, 8192) == 8 and s(4, 32768) == 32   # (as before)
+
+
 def prompt(B, Hq, Hkv, N, d, cap=0.0, slopes=NULL):
     return ("vfa_masked_attn_fwd", [P, P, P, P, P, B, Hq, Hkv, N, d, 1, P, 0.0, cap, slopes, NULL], 0)
 
