@@ -234,6 +234,26 @@ def test_every_row_of_every_head(vfa, B, Hq, Hkv, N, d, parts):
             compare(O[b, mine].reshape(-1, d), lse[b, mine].reshape(-1), *(t.cpu() for t in want), (b, h))
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_longest(vfa, d):
+    """The longest prompt that is taken: a head's keys end one row short of 2^31 bytes.  Windows, so that it takes no time; rows at either end and between."""
+    N = 0x7FFFFFFF // (2 * d)
+    g = torch.Generator("cuda").manual_seed(d)
+    Q, K, V = (torch.randn((1, 1, N, d), generator=g, device="cuda", dtype=torch.bfloat16) for _ in range(3))
+    i = torch.arange(N, device="cuda", dtype=torch.int32)
+    ranges = torch.stack((i - 150, i + 60), -1)[None].contiguous()
+    assert -(-N // 128) >= places(d)
+    O, lse = vfa.masked_attn_fwd(Q, K, V, ranges=ranges, slopes=torch.tensor([0.02], device="cuda"))
+    for r in (0, 127, N // 3, N // 2 + 1, N - 128, N - 40, N - 1):
+        lo, hi = max(0, r - 150), min(N, r + 60)
+        key = torch.arange(lo, hi)
+        seen = torch.ones((1, hi - lo), dtype=torch.bool)
+        want = attend_by_key(Q[0, 0, r: r + 1].cpu(), K[0, 0, lo:hi].cpu(), V[0, 0, lo:hi].cpu(), seen, (r - key).abs().double()[None], 0.0, 0.02)
+        compare(O[0, 0, r: r + 1], lse[0, 0, r: r + 1], *want, r)
+    with pytest.raises(vfa.VfaError):
+        vfa.masked_attn_fwd(*(torch.empty((1, 1, N + 1, d), dtype=torch.bfloat16, device="cuda") for _ in range(3)))
+
+
 def test_replayed(vfa):
     """Captured once and replayed with new inputs and masks, an eager call of the same kind between the replays."""
     N, d = 600, 128
