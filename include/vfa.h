@@ -427,7 +427,8 @@ int vfa_kvp_append(const void* K, const void* V, void* KP, void* VP, const int* 
                    void* stream);
 
 /* A number of key ranges for vfa_kvp_decode_fwd that suits a batch of sequences of n_keys tokens each (varlen = 0), or of lengths of their own up to
- * n_keys (varlen = 1), on the current device. */
+ * n_keys (varlen = 1), on the current device.  What it does not know is how the lengths differ: with many KV heads and a capacity of more than 4096 tokens it allows for
+ * one long sequence among short ones, at up to 7 % for lengths that are even. */
 int vfa_kvp_decode_splits(int B, int Hq, int Hkv, int n_q, int d, int n_keys, int varlen);
 
 /* Bytes of workspace vfa_kvp_decode_fwd needs for n_splits > 1. */
@@ -436,7 +437,8 @@ size_t vfa_kvp_decode_workspace_bytes(int B, int Hq, int n_q, int d, int n_split
 /* Attention of each sequence's n_q newest tokens (1: a decode step; more: drafted tokens, or a piece of a prompt) over its pages, which hold them
  * already.  Q, O [B, Hq, n_q, d] bf16, LSE [B, Hq, n_q] fp32 or NULL.  Sequence b has L = seq_lens[b] tokens (NULL: n_keys); its token t of the n_q has
  * position L - n_q + t and sees the keys up to that one; a token that sees none gives O = 0, LSE = -inf.  What a row does not see does not reach it,
- * infinities and NaN among the values included.  Weights for the product with V are held to 2^-16 where a KV head has up to 16 rows (Hq / Hkv) * n_q, else
+ * infinities and NaN among the values included.  An infinity among the values of a key that it does see gives that infinity, or, with a weight of less than 2^-100 of the row's largest,
+ * that or NaN.  Weights for the product with V are held to 2^-16 where a KV head has up to 16 rows (Hq / Hkv) * n_q, else
  * rounded to bf16.  Hq / Hkv <= 32, else VFA_ERR_UNSUPPORTED; up to 32 rows of a KV head are one workgroup's, more (a prompt in pieces) are cut into groups
  * of whole tokens, which read the pages each.  n_splits and workspace as in vfa_kv8_decode_fwd (1 to 4096; vfa_kvp_decode_splits suggests one; the
  * workspace, 16-byte aligned, contents irrelevant, is used for n_splits > 1 only).  Calls that may run at the same time need workspaces of their own. */
@@ -455,8 +457,10 @@ int vfa_row_ranges(const int* doc_offsets, const int* prefix_lens, int* ranges, 
 /* Attention of whole prompts.  Layouts as above (Q, O [B, Hq, N, d], K, V [B, Hkv, N, d], LSE may be NULL).  Row i of entry b sees the keys
  * ranges[b][i][0] <= j < ranges[b][i][1] (int32 [B, N, 2] on the device, 8-byte aligned, from vfa_row_ranges or any others, e.g. windows; clamped to [0, N];
  * NULL: all keys) and, with causal = 1, of those the ones up to itself; a row that sees none gives O = 0, LSE = -inf.  Positions are i and j.  What a
- * row does not see does not reach it, infinities and NaN included.  Exact attention; weights are rounded to bf16 for the product with V, as in vfa_attn_fwd.  2 * d * N
- * < 2^31, else VFA_ERR_UNSUPPORTED. */
+ * row does not see does not reach it, infinities and NaN included; an infinity among the values of a key that it does see gives that infinity, or, with a weight of less than
+ * 2^-100 of the row's largest, that or NaN.  Exact attention; weights are rounded to bf16 for the product with V, as in vfa_attn_fwd.  2 * d * N < 2^31, else
+ * VFA_ERR_UNSUPPORTED.  (Without ranges, cap and slopes vfa_attn_fwd computes the same attention.  It is faster at d = 128 (32 heads over 8, N = 777 13.0 / 16.5 us, 8192 472 / 508)
+ * and at d = 64 on short prompts (777 10.2 / 11.2); this call is on long ones (4 x 16 heads of 4096 194 / 165).) */
 int vfa_masked_attn_fwd(const void* Q, const void* K, const void* V, void* O, float* LSE, int B, int Hq, int Hkv, int N, int d,
                         int causal, const int* ranges, float softmax_scale, float score_cap, const float* slopes,
                         void* stream);

@@ -540,7 +540,8 @@ def _need(ok, what):
 
 def qk_norm_rope_fwd(q, k, v=None, *, norm=True, q_weight=None, k_weight=None, eps=1e-6, cos_sin=None, interleaved=False, first_pos=0,
                      out=None, stream=None):
-    """Projected q [B, N, Hq, d], k and v [B, N, Hkv, d] (bf16, slices of one projection or any other strides) -> Q [B, Hq, N, d] and
+    """Projected q [B, N, Hq, d], k and v [B, N, Hkv, d] (bf16, slices of one projection or any other strides
+    of whole 16 bytes) -> Q [B, Hq, N, d] and
     K, V [B, Hkv, N, d] as the attention calls take them: queries and keys normed over each head (norm=True; weights [d] or None) and
     rotated by position (cos_sin [n_pos, rot] fp32: cosines, then sines; None: no rotation).  first_pos: position of token 0, a
     number or an int32 tensor of B entries.  out: (Q, K, V) to write to."""
@@ -575,8 +576,8 @@ def kv8_cache(B: int, Hkv: int, n_cap: int, d: int, device=None):
 
 
 def kv8_append(K, V, cache, old_lens, new_lens, stream=None):
-    """Writes rows of K, V [B, Hkv, n_in, d] (bf16, any strides) into the cache, in place, as tokens old_lens <= n < new_lens of each
-    sequence (numbers, or int32 tensors of B entries, both alike)."""
+    """Writes rows of K, V [B, Hkv, n_in, d] (bf16, any strides of whole 16 bytes, from an address that is a multiple of them) into the cache, in place, as tokens
+    old_lens <= n < new_lens of each sequence (numbers, or int32 tensors of B entries, both alike)."""
     n = _ns()
     K8, V8, KS, VS = cache
     dev, *sizes = n.check_kv8_append(K, V, K8, V8, KS, VS, old_lens, new_lens, _bf16, _u8, _i32)
@@ -665,8 +666,8 @@ def kvp_cache(n_pages: int, Hkv: int, page: int, d: int, device=None):
 
 
 def kvp_append(K, V, cache, table, old_lens, new_lens, stream=None):
-    """Writes rows of K, V [B, Hkv, n_in, d] (bf16, any strides) into the pages, in place, as tokens old_lens <= n < new_lens of each sequence (numbers, or
-    int32 tensors of B entries, both alike).  Entries of the table outside the pool take nothing."""
+    """Writes rows of K, V [B, Hkv, n_in, d] (bf16, any strides of whole 16 bytes, from an address that is a multiple of them) into the pages, in place, as tokens
+    old_lens <= n < new_lens of each sequence (numbers, or int32 tensors of B entries, both alike).  Entries of the table outside the pool take nothing."""
     n = _ns()
     KP, VP = cache
     dev, *sizes = n.check_kvp_append(K, V, KP, VP, table, old_lens, new_lens, _bf16, _i32)
@@ -748,7 +749,8 @@ def row_ranges(doc_offsets, N: int, *, prefix_lens=None, causal=True, out=None, 
 def masked_attn_fwd(Q, K, V, *, causal=None, ranges=None, score_cap=0.0, slopes=None, softmax_scale=0.0, out=None, lse=None, want_lse=True, stream=None):
     """Attention of whole prompts, Q [B, Hq, N, d], K and V [B, Hkv, N, d].  ranges (int32 [B, N, 2], see row_ranges): the keys that each row sees; causal: only
     those up to itself (None: causal where there are no ranges, which say all there is to say elsewhere).  score_cap: scores become score_cap * tanh(s /
-    score_cap); slopes (fp32 [Hq]): slope times distance is subtracted.  Returns (O, LSE); rows that see nothing give 0 and -inf."""
+    score_cap); slopes (fp32 [Hq]): slope times distance is subtracted.  Returns (O, LSE); rows that see nothing give 0 and -inf.
+    (Without ranges, cap and slopes vfa_attn_fwd is faster at d = 128, and at d = 64 on short prompts.)"""
     if stream is not None and (out is None or (lse is None and want_lse)):
         return _on(stream, masked_attn_fwd, locals())
     n = _ns()

@@ -37,7 +37,9 @@ __device__ __forceinline__ void bias_scores(const Scores& s, float c, f32x16* st
 }
 
 // Softmax step of one tile, exact running max, the rescale branched over in tiles that do not raise it.  HALVES: the lane's weights without `upper` of
-// their bits, rounded towards zero (what is left of a weight has 16 bits); else rounded to bf16.
+// their bits, rounded towards zero (what is left of a weight has 16 bits); else rounded to bf16, which the matrix unit takes and which costs nothing, where columns are not free for a second
+// half.  (The sum that divides has the weights whole, so with halves an output is low by up to 2^-16 of itself, a 256th of its own rounding, and rounding to the nearest would take an
+// instruction a weight.)
 template <bool HALVES, int DB>
 __device__ __forceinline__ void softmax_halves(f32x16* st, uint32_t* pk, f32x16* ot, float& m2, float& lsum, float c, uint32_t upper) {
     if (!HALVES) {
