@@ -109,7 +109,8 @@ int vfa_kvp_append(const void* K, const void* V, void* KP, void* VP, const int* 
 // More than one and a half heads for each unit keep them busy with one range each if lengths are even, and wait for the longest if they are not.  Which they are is not known here, the
 // capacity is.  Even from 200 up to it / one of it and the others 200, 64 x 8 heads, d = 128: of 2048 1 range 48 / 33, 2 56 / 21, 4 58 / 24; of 4096 86 / 51, 97 / 21, 94 / 24; of 8192 166 / 87,
 // 182 / 23, 175 / 27; of 16384 324 / 160, 349 / 28, 341 / 34 (of 8192 50 x 8 136 / 86, 162 / 22, 145 / 25; 70 x 8 199 / 92, 209 / 25, three 203 / 28, four, not dealt, 199 / 68; d = 64, 64 x 8
-// 94 / 50, 97 / 16, 92 / 16).  So one up to 4096 keys, which one unit reads in 40 us (20 at d = 64), above that up to four while they are dealt.
+// 94 / 50, 97 / 16, 92 / 16).  So one up to 4096 keys, which one unit reads in 40 us (20 at d = 64), above that up to four while there are no
+// more than 1024 heads (64 x 32 of 8192 695 / 136, two 735 / 73; d = 64 321 / 70, 371 / 40) and they are dealt.
 // More than 256 sequences are not dealt, but take more than one range above 2048 keys too (300 heads of 100 to 1000 keys 1 range 18, 3 31; of 4000 58 / 63, all of 4000 121 / 108; one of
 // 32768 and the others 200 288 / 115; 512 of 200 to 8192 168, 2 173, one of 8192 and the others 200 84 / 61).
 int vfa_kvp_decode_splits(int B, int Hq, int Hkv, int n_q, int d, int n_keys, int varlen) {
